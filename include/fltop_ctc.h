@@ -278,6 +278,157 @@ int fltop_ctc_token_ranks(const float* logprobs, int32_t B, int32_t T, int32_t V
 int fltop_ctc_log_add(const double* a, const double* b, double* out, int64_t n,
                       void* hip_stream);
 
+/* ---- Learning from hypotheses --------------------------------------------------------------
+ *
+ * The search answers with hypotheses (the returned prefix, the n-best export); the calls below
+ * say how probable a hypothesis is with nothing pruned, and give the gradients with which a
+ * model learns from them: fltop_ctc_score and fltop_ctc_score_grad between emissions and the
+ * scores of hypotheses, the losses between those scores (or the logits of frames) and one
+ * number.  The conventions above hold: device buffers of the caller, launches on `hip_stream`
+ * only, nothing allocated, kept or synchronised; two calls may overlap if their workspaces and
+ * outputs are different.  Every result is the same bit for bit from call to call (no sum goes
+ * by the order in which threads arrive). */
+
+#define FLTOP_TYPE_F32  0
+#define FLTOP_TYPE_BF16 1
+#define FLTOP_TYPE_F16  2
+
+/* Most tokens a hypothesis may hold in fltop_ctc_score (fltop_hypotheses.U). */
+#define FLTOP_MAX_LABELS 4095
+
+/* Rows of a batch: emissions or logits (host POD, read during the call only). */
+typedef struct fltop_rows {
+    const void*    data;          /* dev [B,T,V] of `type`; the V values of a row are adjacent    */
+    const int32_t* lengths;       /* dev [B], clamped to [0,T]; later frames are never read       */
+    int64_t        batch_stride;  /* elements from an utterance to the next (T * V when dense)    */
+    int64_t        frame_stride;  /* elements from a frame to the next (V when dense)             */
+    int32_t        B, T, V;
+    int32_t        type;          /* FLTOP_TYPE_*                                                 */
+} fltop_rows;
+
+/* Hypotheses of a batch, as the n-best export writes them or as transcripts come (host POD). */
+typedef struct fltop_hypotheses {
+    const int32_t* tokens;        /* dev [B,N,U] the U tokens of a hypothesis adjacent, first
+                                     `lengths` of them used                                       */
+    const int32_t* lengths;       /* dev [B,N] hypotheses of an utterance adjacent                */
+    const int32_t* counts;        /* dev [B] hypotheses of utterance b (clamped to [0,N]), or NULL
+                                     for N each                                                   */
+    int64_t        token_batch_stride;   /* elements from an utterance's tokens to the next's     */
+    int64_t        token_stride;         /* elements from a hypothesis's tokens to the next's     */
+    int64_t        length_batch_stride;  /* elements from an utterance's lengths to the next's    */
+    int32_t        N, U;
+} fltop_hypotheses;
+
+/* Log-probability of hypotheses: out_scores dev [B,N] receives
+ *     ln sum over all alignments pi of y (of lengths[b] frames) of prod_t exp(lp[b,t,pi_t]),
+ * the mass that the search would give prefix y if nothing were pruned and no table were set
+ * (repeats of a token need a blank between them).  The sum is taken in fp64 with exponents kept
+ * apart, so that it neither under- nor overflows.  -inf: the hypothesis has no alignment -- too
+ * few frames, only impossible ones, or a token that is the blank or not below V.  Hypotheses at
+ * or beyond counts[b] and those of negative length are not there: their score is -inf too.  A
+ * hypothesis of more than U tokens is not scored: NaN.  An emission below -7e8 counts as -inf;
+ * NaN and +inf are undefined, as in the decoder.
+ *   workspace  NULL if only the scores are wanted; else dev, 256-byte aligned, of at least
+ *              fltop_ctc_score_workspace_bytes(B, T, N, U) bytes, into which the call puts what
+ *              fltop_ctc_score_grad goes on from.
+ * Refused: B, T, N < 1, V < 2, U < 1 or beyond FLTOP_MAX_LABELS, B * N >= 2^31 (BAD_SHAPE), V >
+ * FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type (BAD_OPTION). */
+size_t fltop_ctc_score_workspace_bytes(int32_t B, int32_t T, int32_t N, int32_t U);
+int fltop_ctc_score(const fltop_rows* logprobs, const fltop_hypotheses* hyps, double* out_scores,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient of a function of those scores to the emissions: grad_scores dev [B,N] is its
+ * derivative to each score, grad_logprobs dev [B,T,V] (dense, of the emissions' type) receives
+ *     sum over n of grad_scores[b,n] * P(pi_t = v | hypothesis n of utterance b, emissions)
+ * and 0 in frames at or beyond lengths[b].  Hypotheses without a finite score take no part,
+ * whatever their grad_scores.  `workspace` as fltop_ctc_score left it for the same emissions and
+ * hypotheses; it may be used for any number of gradients.  Emissions are taken as they are given:
+ * where they come from a log-softmax, its own gradient follows.  Occupancies are summed as whole
+ * multiples of 2^-50 of the utterance's largest |grad_scores|. */
+int fltop_ctc_score_grad(const fltop_rows* logprobs, const fltop_hypotheses* hyps,
+                         const double* grad_scores, void* workspace, size_t workspace_bytes,
+                         void* grad_logprobs, void* hip_stream);
+
+/* Preference loss over pairs of an utterance's hypotheses: with s the scores and q the reference
+ * model's (0 where ref_scores is NULL), a pair (won, lost) has the margin
+ *     h = (s[won] - s[lost]) - (q[won] - q[lost])
+ * and the loss
+ *     FLTOP_PREFERENCE_SIGMOID  -(1 - label_smoothing) ln sigma(beta h)
+ *                               - label_smoothing ln sigma(-beta h)
+ *     FLTOP_PREFERENCE_HINGE    max(0, 1 - beta h)
+ *     FLTOP_PREFERENCE_SQUARE   (h - 1 / (2 beta))^2
+ * The result is the mean over the pairs that take part: those before pair_counts[b] whose two
+ * indices are in [0,N) and whose scores are all finite.  A pair may appear twice (it counts
+ * twice) and hypotheses may be shared by pairs (their gradients add up).  No pair: loss 0. */
+#define FLTOP_PREFERENCE_SIGMOID 0
+#define FLTOP_PREFERENCE_HINGE   1
+#define FLTOP_PREFERENCE_SQUARE  2
+typedef struct fltop_preference {
+    const double*  scores;        /* dev [B,N]                                                    */
+    const double*  ref_scores;    /* dev [B,N] or NULL                                            */
+    const int32_t* pairs;         /* dev [B,M,2] (won, lost)                                      */
+    const int32_t* pair_counts;   /* dev [B] (clamped to [0,M]) or NULL for M each                */
+    int32_t        B, N, M;       /* N up to FLTOP_MAX_BEAM                                       */
+    int32_t        kind;          /* FLTOP_PREFERENCE_*                                           */
+    double         beta;          /* > 0                                                          */
+    double         label_smoothing; /* [0, 0.5], sigmoid only (else 0)                            */
+    double         scale;         /* the gradient is that of scale * loss                         */
+    double*        loss;          /* dev [1]                                                      */
+    double*        margins;       /* dev [B,M]: h, NaN for pairs that take no part                */
+    double*        grad_scores;   /* dev [B,N]                                                    */
+} fltop_preference;
+size_t fltop_preference_workspace_bytes(int32_t B);
+int fltop_preference_loss(const fltop_preference* p, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+
+/* Clipped policy loss: with l a log-probability under the model, l_old under the model that made
+ * the samples, l_ref under a reference model, A the advantage, r = exp(l - l_old),
+ *     f  = max(-A r, -A min(max(r, 1 - clip_low), 1 + clip_high)) + kl_weight * kl
+ *     kl = exp(l_ref - l) - (l_ref - l) - 1                    (0 without a reference)
+ * reduced over everything that takes part: FLTOP_REDUCE_TOKEN the mean of all, _SEQUENCE the
+ * mean over the rows b (that have any) of each row's mean, _SUM the sum.  The gradient goes
+ * through r where A r is not above its clipped value.  Nothing takes part: 0. */
+#define FLTOP_REDUCE_TOKEN    0
+#define FLTOP_REDUCE_SEQUENCE 1
+#define FLTOP_REDUCE_SUM      2
+typedef struct fltop_policy {
+    int32_t reduction;            /* FLTOP_REDUCE_*                                               */
+    int32_t reserved;             /* set to 0                                                     */
+    double  clip_low;             /* [0, 1]                                                       */
+    double  clip_high;            /* >= 0                                                         */
+    double  kl_weight;
+    double  scale;                /* the gradient is that of scale * loss                         */
+} fltop_policy;
+size_t fltop_policy_workspace_bytes(int32_t B, int32_t T);
+
+/* The loss over log-probabilities that the caller has (hypotheses: fltop_ctc_score's [B,N]):
+ *   scores, old_scores, ref_scores (or NULL), advantages   dev [B,N]
+ *   counts       dev [B] entries of row b (clamped to [0,N]) or NULL
+ *   summary      dev [3]: loss, kl (reduced alike), share of entries whose ratio was clipped
+ *   grad_scores  dev [B,N], 0 for entries that take no part
+ * An entry takes part if it is before counts[b] and its numbers are all finite.
+ * workspace: fltop_policy_workspace_bytes(B, 1) bytes, 256-byte aligned. */
+int fltop_policy_loss(const double* scores, const double* old_scores, const double* ref_scores,
+                      const double* advantages, const int32_t* counts, int32_t B, int32_t N,
+                      const fltop_policy* policy, void* workspace, size_t workspace_bytes,
+                      double* summary, double* grad_scores, void* hip_stream);
+
+/* The loss over frames (or the tokens of a text): l = log-softmax(logits[b,t])[tokens[b,t]].
+ *   tokens      dev [B,T]; a frame takes part if it is before lengths[b] and its token in [0,V),
+ *               so a prompt or padding is left out by -1
+ *   old_logps, ref_logps (or NULL)   dev [B,T] fp32
+ *   advantages  dev [B], or [B,T] if advantages_per_frame is not 0
+ *   summary     dev [3] fp32 as above
+ *   logps       dev [B,T] fp32: l, 0 where no part is taken
+ *   grad_logits dev [B,T,V] (dense, of the logits' type), 0 in frames that take no part
+ * Softmax statistics are fp32, logarithms and the loss of a frame fp64.  Any V >= 1.
+ * workspace: fltop_policy_workspace_bytes(B, T) bytes, 256-byte aligned. */
+int fltop_policy_loss_logits(const fltop_rows* logits, const int32_t* tokens,
+                             const float* old_logps, const float* ref_logps,
+                             const float* advantages, int32_t advantages_per_frame,
+                             const fltop_policy* policy, void* workspace, size_t workspace_bytes,
+                             float* summary, float* logps, void* grad_logits, void* hip_stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* fltop_status_string(int status);
 

@@ -27,7 +27,12 @@ EXPORTS = ("fltop_ctc_workspace_bytes", "fltop_ctc_workspace_bytes_for", "fltop_
            "fltop_ctc_prune", "fltop_ctc_search",
            "fltop_ctc_unpack_survivors", "fltop_ctc_token_ranks", "fltop_ctc_stream_state_bytes",
            "fltop_ctc_stream_begin", "fltop_ctc_stream_decode", "fltop_ctc_log_add",
+           "fltop_ctc_score_workspace_bytes", "fltop_ctc_score", "fltop_ctc_score_grad",
+           "fltop_preference_workspace_bytes", "fltop_preference_loss",
+           "fltop_policy_workspace_bytes", "fltop_policy_loss", "fltop_policy_loss_logits",
            "fltop_status_string")
+
+MAX_LABELS = 4095             # tokens of a hypothesis in ctc_score
 
 
 class FltopParams(ctypes.Structure):
@@ -47,6 +52,62 @@ class FltopParams(ctypes.Structure):
         ("nbest_pnb", ctypes.c_void_p),
         ("frame_beam", ctypes.c_void_p),
         ("out_token_frames", ctypes.c_void_p),
+    ]
+
+
+class FltopRows(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("lengths", ctypes.c_void_p),
+        ("batch_stride", ctypes.c_int64),
+        ("frame_stride", ctypes.c_int64),
+        ("B", ctypes.c_int32),
+        ("T", ctypes.c_int32),
+        ("V", ctypes.c_int32),
+        ("type", ctypes.c_int32),
+    ]
+
+
+class FltopHypotheses(ctypes.Structure):
+    _fields_ = [
+        ("tokens", ctypes.c_void_p),
+        ("lengths", ctypes.c_void_p),
+        ("counts", ctypes.c_void_p),
+        ("token_batch_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+        ("length_batch_stride", ctypes.c_int64),
+        ("N", ctypes.c_int32),
+        ("U", ctypes.c_int32),
+    ]
+
+
+class FltopPreference(ctypes.Structure):
+    _fields_ = [
+        ("scores", ctypes.c_void_p),
+        ("ref_scores", ctypes.c_void_p),
+        ("pairs", ctypes.c_void_p),
+        ("pair_counts", ctypes.c_void_p),
+        ("B", ctypes.c_int32),
+        ("N", ctypes.c_int32),
+        ("M", ctypes.c_int32),
+        ("kind", ctypes.c_int32),
+        ("beta", ctypes.c_double),
+        ("label_smoothing", ctypes.c_double),
+        ("scale", ctypes.c_double),
+        ("loss", ctypes.c_void_p),
+        ("margins", ctypes.c_void_p),
+        ("grad_scores", ctypes.c_void_p),
+    ]
+
+
+class FltopPolicy(ctypes.Structure):
+    _fields_ = [
+        ("reduction", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("clip_low", ctypes.c_double),
+        ("clip_high", ctypes.c_double),
+        ("kl_weight", ctypes.c_double),
+        ("scale", ctypes.c_double),
     ]
 
 
@@ -104,6 +165,25 @@ def load():
                                             vp, sz, vp, sz, i32, vp, vp, vp, vp, vp]
     lib.fltop_ctc_log_add.restype = ctypes.c_int
     lib.fltop_ctc_log_add.argtypes = [vp, vp, vp, ctypes.c_int64, vp]
+    rows, hyps = ctypes.POINTER(FltopRows), ctypes.POINTER(FltopHypotheses)
+    policy = ctypes.POINTER(FltopPolicy)
+    lib.fltop_ctc_score_workspace_bytes.restype = sz
+    lib.fltop_ctc_score_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.fltop_ctc_score.restype = ctypes.c_int
+    lib.fltop_ctc_score.argtypes = [rows, hyps, vp, vp, sz, vp]
+    lib.fltop_ctc_score_grad.restype = ctypes.c_int
+    lib.fltop_ctc_score_grad.argtypes = [rows, hyps, vp, vp, sz, vp, vp]
+    lib.fltop_preference_workspace_bytes.restype = sz
+    lib.fltop_preference_workspace_bytes.argtypes = [i32]
+    lib.fltop_preference_loss.restype = ctypes.c_int
+    lib.fltop_preference_loss.argtypes = [ctypes.POINTER(FltopPreference), vp, sz, vp]
+    lib.fltop_policy_workspace_bytes.restype = sz
+    lib.fltop_policy_workspace_bytes.argtypes = [i32, i32]
+    lib.fltop_policy_loss.restype = ctypes.c_int
+    lib.fltop_policy_loss.argtypes = [vp, vp, vp, vp, vp, i32, i32, policy, vp, sz, vp, vp, vp]
+    lib.fltop_policy_loss_logits.restype = ctypes.c_int
+    lib.fltop_policy_loss_logits.argtypes = [rows, vp, vp, vp, vp, i32, policy, vp, sz, vp, vp, vp,
+                                             vp]
     lib.fltop_status_string.restype = ctypes.c_char_p
     lib.fltop_status_string.argtypes = [ctypes.c_int]
     _lib = lib
@@ -378,3 +458,243 @@ def stats_dict(stats: torch.Tensor) -> dict:
     out = dict(zip(STATS_FIELDS, vals))
     out.update({f"clk{i}": v for i, v in enumerate(vals[len(STATS_FIELDS):])})
     return out
+
+
+# ---- learning from hypotheses ------------------------------------------------------------------
+
+ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+PREFERENCE_KINDS = {"sigmoid": 0, "hinge": 1, "square": 2}
+REDUCTIONS = {"token": 0, "sequence": 1, "sum": 2}
+
+
+class _On:
+    """The device of `t` made current, and outputs and workspaces taken on the stream that the call
+    is enqueued on, so that they outlive their use there.  `stream` None: that device's current one."""
+
+    def __init__(self, t: torch.Tensor, stream):
+        self._device = t.device if t.device.index != torch.cuda.current_device() else None
+        self._stream = stream
+        self._entered = []
+
+    def __enter__(self):
+        for manager in (self._device and torch.cuda.device(self._device),
+                        self._stream and torch.cuda.stream(self._stream)):
+            if manager is not None:
+                manager.__enter__()
+                self._entered.append(manager)
+        return _stream_handle(self._stream)
+
+    def __exit__(self, *what):
+        while self._entered:
+            self._entered.pop().__exit__(*what)
+
+
+def _need(ok: bool, message: str):
+    if not ok:
+        raise ValueError(message)
+
+
+def _device_tensor(t, name: str, dtype, shape, device):
+    """Checks a dense tensor of one call (all of a call's tensors are on one device)."""
+    if not (t.is_cuda and t.device == device):
+        raise ValueError(f"{name} must be on {device}, where the call's other tensors are")
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
+
+
+def _rows(x: torch.Tensor, lengths: torch.Tensor, name: str) -> FltopRows:
+    _need(x.is_cuda, f"{name} must be a device tensor")
+    _need(x.dtype in ROW_TYPES, f"{name} must be float32, bfloat16 or float16")
+    _need(x.dim() == 3 and x.numel() > 0, f"{name} must be a [B,T,V] tensor")
+    B, T, V = x.shape
+    _need(x.stride(2) == 1 or V == 1, f"{name}: the V values of a row must be adjacent")
+    _device_tensor(lengths, "lengths", torch.int32, (B,), x.device)
+    return FltopRows(x.data_ptr(), lengths.data_ptr(), x.stride(0), x.stride(1), B, T, V,
+                     ROW_TYPES[x.dtype])
+
+
+def _hypotheses(tokens, token_lengths, counts, B: int, device) -> FltopHypotheses:
+    _need(tokens.dim() == 3 and tokens.shape[0] == B and tokens.numel() > 0
+          and tokens.dtype == torch.int32 and tokens.device == device,
+          f"tokens must be an int32 [B,N,U] tensor on {device}")
+    _, N, U = tokens.shape
+    _need(tokens.stride(2) == 1 or U == 1, "the tokens of a hypothesis must be adjacent")
+    _need(tuple(token_lengths.shape) == (B, N) and token_lengths.dtype == torch.int32
+          and token_lengths.device == device, f"token_lengths must be an int32 [B,N] tensor on {device}")
+    _need(token_lengths.stride(1) == 1 or N == 1, "the token lengths of an utterance must be adjacent")
+    if counts is not None:
+        _device_tensor(counts, "counts", torch.int32, (B,), device)
+    return FltopHypotheses(tokens.data_ptr(), token_lengths.data_ptr(),
+                           None if counts is None else counts.data_ptr(), tokens.stride(0),
+                           tokens.stride(1), token_lengths.stride(0), N, U)
+
+
+def _raise(rc: int, where: str):
+    if rc != 0:
+        raise FltopError(rc, where)
+
+
+def _workspace(workspace, nbytes: int, where: str, device) -> torch.Tensor:
+    if nbytes == 0:
+        raise FltopError(-2, where)
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _need(workspace.device == device and workspace.is_contiguous() and workspace.dtype == torch.uint8,
+          f"the workspace must be a contiguous uint8 tensor on {device}")
+    return workspace
+
+
+def score_workspace_bytes(B: int, T: int, N: int, U: int) -> int:
+    """Bytes that ctc_score leaves for ctc_score_grad (0 if the shapes are invalid)."""
+    return int(load().fltop_ctc_score_workspace_bytes(B, T, N, U))
+
+
+def ctc_score(logprobs: torch.Tensor, lengths: torch.Tensor, tokens: torch.Tensor,
+              token_lengths: torch.Tensor, counts: Optional[torch.Tensor] = None, *,
+              want_grad: bool = False, workspace: Optional[torch.Tensor] = None,
+              stream=None) -> dict:
+    """fltop_ctc_score: log-probability of N hypotheses of each utterance, over all alignments.
+
+    logprobs [B,T,V] float32, bfloat16 or float16 with adjacent values in a row (a [T,B,V] tensor
+    transposed is fine), lengths [B]; tokens [B,N,U] and token_lengths [B,N] int32 as decode's
+    n-best export gives them (slices too: `nbest_tokens[:, :8, :200]`), counts [B] its nbest_count.
+    Returns scores [B,N] float64; with want_grad also the workspace that ctc_score_grad needs
+    (about 24 * B * N * T * U bytes: slice the tokens to the longest hypothesis)."""
+    x = _rows(logprobs, lengths, "logprobs")
+    dev = logprobs.device
+    h = _hypotheses(tokens, token_lengths, counts, x.B, dev)
+    with _On(logprobs, stream) as handle:
+        out = {"scores": torch.empty((x.B, h.N), dtype=torch.float64, device=dev)}
+        if want_grad or workspace is not None:
+            out["workspace"] = _workspace(workspace, score_workspace_bytes(x.B, x.T, h.N, h.U),
+                                          "fltop_ctc_score_workspace_bytes", dev)
+        ws = out.get("workspace")
+        _raise(load().fltop_ctc_score(ctypes.byref(x), ctypes.byref(h), _ptr(out["scores"]), _ptr(ws),
+                                      0 if ws is None else ws.numel(), handle), "fltop_ctc_score")
+    return out
+
+
+def ctc_score_grad(logprobs: torch.Tensor, lengths: torch.Tensor, tokens: torch.Tensor,
+                   token_lengths: torch.Tensor, grad_scores: torch.Tensor,
+                   workspace: torch.Tensor, counts: Optional[torch.Tensor] = None, *,
+                   stream=None) -> torch.Tensor:
+    """fltop_ctc_score_grad: from the derivative of a loss to ctc_score's scores (float64 [B,N])
+    its derivative to logprobs, [B,T,V] of their type.  The other arguments as given to ctc_score,
+    `workspace` as it returned it.  A model's gradient follows by `logprobs.backward(grad)`."""
+    x = _rows(logprobs, lengths, "logprobs")
+    dev = logprobs.device
+    h = _hypotheses(tokens, token_lengths, counts, x.B, dev)
+    _device_tensor(grad_scores, "grad_scores", torch.float64, (x.B, h.N), dev)
+    ws = _workspace(workspace, score_workspace_bytes(x.B, x.T, h.N, h.U), "fltop_ctc_score_workspace_bytes", dev)
+    with _On(logprobs, stream) as handle:
+        grad = torch.empty((x.B, x.T, x.V), dtype=logprobs.dtype, device=dev)
+        _raise(load().fltop_ctc_score_grad(ctypes.byref(x), ctypes.byref(h), _ptr(grad_scores), _ptr(ws),
+                                           ws.numel(), _ptr(grad), handle), "fltop_ctc_score_grad")
+    return grad
+
+
+def preference_loss(scores: torch.Tensor, pairs: torch.Tensor, *,
+                    ref_scores: Optional[torch.Tensor] = None,
+                    pair_counts: Optional[torch.Tensor] = None, kind: str = "sigmoid",
+                    beta: float = 0.1, label_smoothing: float = 0.0, scale: float = 1.0,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """fltop_preference_loss: mean loss over pairs (won, lost) of an utterance's hypotheses.
+
+    scores, ref_scores float64 [B,N] (ctc_score's), pairs int32 [B,M,2] of places in [0,N) (a pair
+    with any other place takes no part), pair_counts int32 [B]; kind "sigmoid", "hinge" or "square".
+    Returns loss (float64), margins [B,M] and grad_scores [B,N], the gradient of scale * loss."""
+    _need(scores.is_cuda and scores.dim() == 2, "scores must be a [B,N] device tensor")
+    dev, (B, N) = scores.device, scores.shape
+    _device_tensor(scores, "scores", torch.float64, (B, N), dev)
+    _need(pairs.dim() == 3, "pairs must be an int32 [B,M,2] tensor")
+    M = pairs.shape[1]
+    _device_tensor(pairs, "pairs", torch.int32, (B, M, 2), dev)
+    if ref_scores is not None:
+        _device_tensor(ref_scores, "ref_scores", torch.float64, (B, N), dev)
+    if pair_counts is not None:
+        _device_tensor(pair_counts, "pair_counts", torch.int32, (B,), dev)
+    _need(kind in PREFERENCE_KINDS, f"kind must be one of {', '.join(PREFERENCE_KINDS)}")
+    with _On(scores, stream) as handle:
+        grad = torch.empty_like(scores)
+        loss = torch.empty((), dtype=torch.float64, device=dev)
+        margins = torch.empty((B, M), dtype=torch.float64, device=dev)
+        ws = _workspace(workspace, int(load().fltop_preference_workspace_bytes(B)),
+                        "fltop_preference_workspace_bytes", dev)
+        p = FltopPreference(scores.data_ptr(), None if ref_scores is None else ref_scores.data_ptr(),
+                            pairs.data_ptr(), None if pair_counts is None else pair_counts.data_ptr(),
+                            B, N, M, PREFERENCE_KINDS[kind], beta, label_smoothing, scale,
+                            loss.data_ptr(), margins.data_ptr(), grad.data_ptr())
+        _raise(load().fltop_preference_loss(ctypes.byref(p), _ptr(ws), ws.numel(), handle),
+               "fltop_preference_loss")
+    return {"loss": loss, "margins": margins, "grad_scores": grad}
+
+
+def _policy(reduction, clip_low, clip_high, kl_weight, scale) -> FltopPolicy:
+    _need(reduction in REDUCTIONS, f"reduction must be one of {', '.join(REDUCTIONS)}")
+    return FltopPolicy(REDUCTIONS[reduction], 0, clip_low, clip_high, kl_weight, scale)
+
+
+def policy_loss(scores: torch.Tensor, old_scores: torch.Tensor, advantages: torch.Tensor, *,
+                ref_scores: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+                clip_low: float = 0.2, clip_high: float = 0.2, kl_weight: float = 0.0,
+                reduction: str = "token", scale: float = 1.0,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """fltop_policy_loss: clipped policy loss with a KL term over log-probabilities, float64 [B,N]
+    throughout (ctc_score's scores of an utterance's hypotheses); counts int32 [B].  `reduction`
+    "token" (mean of all entries), "sequence" (mean of the rows' means) or "sum".  Returns loss, kl,
+    clipped (share of entries) and grad_scores [B,N], the gradient of scale * loss."""
+    _need(scores.is_cuda and scores.dim() == 2, "scores must be a [B,N] device tensor")
+    dev, (B, N) = scores.device, scores.shape
+    for name, t in (("scores", scores), ("old_scores", old_scores), ("advantages", advantages),
+                    ("ref_scores", ref_scores)):
+        if t is not None:
+            _device_tensor(t, name, torch.float64, (B, N), dev)
+    if counts is not None:
+        _device_tensor(counts, "counts", torch.int32, (B,), dev)
+    p = _policy(reduction, clip_low, clip_high, kl_weight, scale)
+    with _On(scores, stream) as handle:
+        grad = torch.empty_like(scores)
+        summary = torch.empty(3, dtype=torch.float64, device=dev)
+        ws = _workspace(workspace, int(load().fltop_policy_workspace_bytes(B, 1)),
+                        "fltop_policy_workspace_bytes", dev)
+        _raise(load().fltop_policy_loss(_ptr(scores), _ptr(old_scores), _ptr(ref_scores), _ptr(advantages),
+                                        _ptr(counts), B, N, ctypes.byref(p), _ptr(ws), ws.numel(),
+                                        _ptr(summary), _ptr(grad), handle), "fltop_policy_loss")
+    loss, kl, clipped = summary.unbind()
+    return {"loss": loss, "kl": kl, "clipped": clipped, "grad_scores": grad}
+
+
+def policy_loss_logits(logits: torch.Tensor, tokens: torch.Tensor, lengths: torch.Tensor,
+                       old_logps: torch.Tensor, advantages: torch.Tensor, *,
+                       ref_logps: Optional[torch.Tensor] = None, clip_low: float = 0.2,
+                       clip_high: float = 0.2, kl_weight: float = 0.0, reduction: str = "token",
+                       scale: float = 1.0, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> dict:
+    """fltop_policy_loss_logits: the same loss over the frames (or tokens) of [B,T,V] logits.
+
+    logits float32, bfloat16 or float16 with adjacent values in a row, tokens int32 [B,T] (a place
+    with a token outside [0,V), such as -1, takes no part), lengths int32 [B], old_logps and
+    ref_logps float32 [B,T], advantages float32 [B] or [B,T].  Returns loss, kl, clipped, logps
+    [B,T] float32 and grad_logits [B,T,V] of the logits' type, the gradient of scale * loss."""
+    x = _rows(logits, lengths, "logits")
+    dev, shape = logits.device, (x.B, x.T)
+    _device_tensor(tokens, "tokens", torch.int32, shape, dev)
+    _device_tensor(old_logps, "old_logps", torch.float32, shape, dev)
+    if ref_logps is not None:
+        _device_tensor(ref_logps, "ref_logps", torch.float32, shape, dev)
+    per_frame = advantages.dim() == 2
+    _device_tensor(advantages, "advantages", torch.float32, shape if per_frame else (x.B,), dev)
+    p = _policy(reduction, clip_low, clip_high, kl_weight, scale)
+    with _On(logits, stream) as handle:
+        grad = torch.empty((x.B, x.T, x.V), dtype=logits.dtype, device=dev)
+        logps = torch.empty(shape, dtype=torch.float32, device=dev)
+        summary = torch.empty(3, dtype=torch.float32, device=dev)
+        ws = _workspace(workspace, int(load().fltop_policy_workspace_bytes(x.B, x.T)),
+                        "fltop_policy_workspace_bytes", dev)
+        _raise(load().fltop_policy_loss_logits(ctypes.byref(x), _ptr(tokens), _ptr(old_logps),
+                                               _ptr(ref_logps), _ptr(advantages), int(per_frame),
+                                               ctypes.byref(p), _ptr(ws), ws.numel(), _ptr(summary),
+                                               _ptr(logps), _ptr(grad), handle),
+               "fltop_policy_loss_logits")
+    loss, kl, clipped = summary.unbind()
+    return {"loss": loss, "kl": kl, "clipped": clipped, "logps": logps, "grad_logits": grad}

@@ -1,0 +1,130 @@
+// Shared by the operators that learn from hypotheses: element types, numbers with an exponent of
+// their own, and the launchers of the kernels.
+#ifndef FLTOP_LEARN_H_
+#define FLTOP_LEARN_H_
+
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+
+#include "fltop_internal.h"
+
+namespace fltop {
+
+__device__ inline float to_float(float x) { return x; }
+__device__ inline float to_float(__hip_bfloat16 x) { return __bfloat162float(x); }
+__device__ inline float to_float(__half x) { return __half2float(x); }
+
+template <typename T> __device__ inline T from_float(float x);
+template <> __device__ inline float from_float<float>(float x) { return x; }
+template <> __device__ inline __hip_bfloat16 from_float<__hip_bfloat16>(float x) { return __float2bfloat16(x); }
+template <> __device__ inline __half from_float<__half>(float x) { return __float2half(x); }
+
+// A probability mass m * 2^e with m in [1/2, 1), or (0, kNoMass).  The masses of a lattice of a
+// thousand frames lie anywhere between 1 and e^-100000, and one that looks negligible beside the
+// others of its frame may be the only one the hypothesis can end with: each has its own exponent.
+struct Mass {
+    double m;
+    int32_t e;
+};
+constexpr int32_t kNoMass = -(1 << 30);
+
+__device__ inline Mass no_mass() { return {0.0, kNoMass}; }
+__device__ inline Mass unit_mass() { return {0.5, 1}; }
+
+// x * 2^e as a Mass.
+__device__ inline Mass normalized(double x, int32_t e) {
+    const int32_t n = e + __builtin_amdgcn_frexp_exp(x);
+    if (x == 0.0 || n <= kNoMass) return no_mass();
+    return {__builtin_amdgcn_frexp_mant(x), min(n, -kNoMass)};
+}
+
+// exp(lp): lp = k ln2 + r with |r| <= ln2 / 2, the mantissa from the series of e^r (the remainder
+// after r^12 / 12! is below 2^-52).  An lp below -7e8 has no mass, so that exponents (below 2^30 in
+// size here) can be added in 32 bits.
+constexpr float kLeastLogprob = -7e8f;
+__device__ inline Mass mass_of(float lp) {
+    if (lp < kLeastLogprob) return no_mass();
+    const double x = lp > -kLeastLogprob ? (double)-kLeastLogprob : (double)lp;
+    const double k = rint(x * 1.4426950408889634);
+    double r = fma(-k, 0.6931471805599453, x);
+    r = fma(-k, 2.3190468138462996e-17, r);
+    double p = 1.0 / 479001600.0;
+    p = fma(p, r, 1.0 / 39916800.0);
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    return {p, (int32_t)k};  // p in [0.7, 1.42): used as a factor, which need not be normalized
+}
+
+__device__ inline double ln_of(Mass x) {
+    return x.e <= kNoMass ? -INFINITY : fma((double)x.e, 0.6931471805599453, log(x.m));
+}
+
+// Sums in which the terms keep their own exponents until they are aligned to the largest.
+__device__ inline Mass plus(Mass a, Mass b) {
+    const int32_t e = max(a.e, b.e);
+    return {ldexp(a.m, a.e - e) + ldexp(b.m, b.e - e), e};  // not normalized
+}
+
+// A Mass as the lattice keeps it for the gradient, which is fp32.
+struct alignas(8) Mass32 {
+    float m;
+    int32_t e;
+};
+
+// What fltop_ctc_score leaves for fltop_ctc_score_grad.  The states of a hypothesis of L tokens are
+// its L + 1 blanks (places 0..L of a row) and its tokens (from place U + 1 on).
+struct ScoreSpace {
+    double* total_m;   // [B*N] P(hypothesis) as a Mass; kNoMass for one that takes no part
+    int32_t* total_e;  // [B*N]
+    Mass32* rows;      // [B*N][T][row] masses of the alignments up to a state
+    float* shares;     // [B*N][T][row] occupancies
+    int64_t row;       // 2U + 1
+    size_t bytes;
+};
+
+inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32_t U) {
+    ScoreSpace s;
+    const size_t hyps = (size_t)B * (size_t)N;
+    s.row = 2 * (int64_t)U + 1;
+    const size_t off_e = align_up(hyps * sizeof(double), 256);
+    const size_t off_rows = off_e + align_up(hyps * sizeof(int32_t), 256);
+    const size_t places = hyps * (size_t)T * (size_t)s.row;
+    const size_t off_shares = off_rows + align_up(places * sizeof(Mass32), 256);
+    s.bytes = off_shares + align_up(places * sizeof(float), 256);
+    char* p = static_cast<char*>(base);
+    s.total_m = p ? reinterpret_cast<double*>(p) : nullptr;
+    s.total_e = p ? reinterpret_cast<int32_t*>(p + off_e) : nullptr;
+    s.rows = p ? reinterpret_cast<Mass32*>(p + off_rows) : nullptr;
+    s.shares = p ? reinterpret_cast<float*>(p + off_shares) : nullptr;
+    return s;
+}
+
+// Workspace of the policy losses: the sums of each row of the batch, then three numbers a frame.
+inline size_t policy_sums_bytes(int32_t B) { return align_up((size_t)B * 4 * sizeof(double), 256); }
+
+hipError_t launch_score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores,
+                        const ScoreSpace* keep, hipStream_t stream);
+hipError_t launch_score_grad(const fltop_rows& x, const fltop_hypotheses& h,
+                             const double* grad_scores, const ScoreSpace& ws, void* grad,
+                             hipStream_t stream);
+hipError_t launch_preference(const fltop_preference& p, void* workspace, hipStream_t stream);
+hipError_t launch_policy(const double* scores, const double* old_scores, const double* ref_scores,
+                         const double* advantages, const int32_t* counts, int32_t B, int32_t N,
+                         const fltop_policy& policy, void* workspace, double* summary,
+                         double* grad_scores, hipStream_t stream);
+hipError_t launch_policy_logits(const fltop_rows& x, const int32_t* tokens, const float* old_logps,
+                                const float* ref_logps, const float* advantages, bool per_frame,
+                                const fltop_policy& policy, void* workspace, float* summary,
+                                float* logps, void* grad, hipStream_t stream);
+
+}  // namespace fltop
+#endif  // FLTOP_LEARN_H_
