@@ -74,22 +74,24 @@ __device__ inline Mass plus(Mass a, Mass b) {
     return {ldexp(a.m, a.e - e) + ldexp(b.m, b.e - e), e};  // not normalized
 }
 
-// A Mass as the lattice keeps it for the gradient, which is fp32.
-struct alignas(8) Mass32 {
-    float m;
-    int32_t e;
-};
+constexpr int kMostWaves = 8;             // wavefronts that one direction of a lattice takes
+constexpr int kShareBlanks = kMostWaves;  // places for the blanks' occupancy behind a frame's tokens
 
 // What fltop_ctc_score leaves for fltop_ctc_score_grad.  The states of a hypothesis of L tokens are
 // its L + 1 blanks (places 0..L of a row) and its tokens (from place U + 1 on).
 struct ScoreSpace {
     double* total_m;   // [B*N] P(hypothesis) as a Mass; kNoMass for one that takes no part
     int32_t* total_e;  // [B*N]
-    Mass32* rows;      // [B*N][T][row] masses of the alignments up to a state
-    float* shares;     // [B*N][T][row] occupancies
+    double* rows;      // [B*N][T][row] masses of the alignments up to a state, without their exponents
+    int32_t* exps;     // [B*N][blocks of frames][row] those exponents
+    float* shares;     // [B*N][T][U + kShareBlanks] occupancies of the tokens, then of all blanks in parts
     int64_t row;       // 2U + 1
     size_t bytes;
 };
+
+// Frames that are gone through together (8, or 4 where a lane holds many pairs): exponents are kept once for each.
+__host__ __device__ inline int64_t blocks_of(int32_t T, int32_t R) { return ((int64_t)T + R - 1) / R; }
+constexpr int kShortBlocksFrom = 512;   // tokens
 
 inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32_t U) {
     ScoreSpace s;
@@ -98,12 +100,15 @@ inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32
     const size_t off_e = align_up(hyps * sizeof(double), 256);
     const size_t off_rows = off_e + align_up(hyps * sizeof(int32_t), 256);
     const size_t places = hyps * (size_t)T * (size_t)s.row;
-    const size_t off_shares = off_rows + align_up(places * sizeof(Mass32), 256);
-    s.bytes = off_shares + align_up(places * sizeof(float), 256);
+    const size_t off_exps = off_rows + align_up(places * sizeof(double), 256);
+    const size_t blocks = (size_t)blocks_of(T, U < kShortBlocksFrom ? 8 : 4);
+    const size_t off_shares = off_exps + align_up(hyps * blocks * (size_t)s.row * sizeof(int32_t), 256);
+    s.bytes = off_shares + align_up(hyps * (size_t)T * (size_t)(U + kShareBlanks) * sizeof(float), 256);
     char* p = static_cast<char*>(base);
     s.total_m = p ? reinterpret_cast<double*>(p) : nullptr;
     s.total_e = p ? reinterpret_cast<int32_t*>(p + off_e) : nullptr;
-    s.rows = p ? reinterpret_cast<Mass32*>(p + off_rows) : nullptr;
+    s.rows = p ? reinterpret_cast<double*>(p + off_rows) : nullptr;
+    s.exps = p ? reinterpret_cast<int32_t*>(p + off_exps) : nullptr;
     s.shares = p ? reinterpret_cast<float*>(p + off_shares) : nullptr;
     return s;
 }
