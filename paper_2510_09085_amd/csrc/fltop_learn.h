@@ -84,26 +84,35 @@ struct ScoreSpace {
     int32_t* total_e;  // [B*N]
     double* rows;      // [B*N][T][row] masses of the alignments up to a state, without their exponents
     int32_t* exps;     // [B*N][blocks of frames][row] those exponents
-    float* shares;     // [B*N][T][U + kShareBlanks] occupancies of the tokens, then of all blanks in parts
-    int64_t row;       // 2U + 1
+    float* shares;     // [B*N][T][share_row] occupancies of the tokens, then of all blanks in parts
+    int64_t row;       // 2U + 1, and a place for what has no meaning
     size_t bytes;
 };
 
-// Frames that are gone through together (8, or 4 where a lane holds many pairs): exponents are kept once for each.
+// Pairs of states that a lane holds: as few as keep a direction within two wavefronts, so that each of a
+// workgroup's wavefronts has a SIMD for itself (eight of eight pairs beyond 1023 tokens).
+inline int lattice_pairs(int32_t B, int32_t N, int32_t U) {
+    (void)B, (void)N;
+    return U < 128 ? 1 : U < 256 ? 2 : U < 512 ? 4 : 8;
+}
+inline int waves_for(int32_t U, int pairs) { return (U + 64 * pairs) / (64 * pairs); }   // for U + 1 pairs
+// Frames that are gone through together: exponents are kept once for each such block.
+inline int block_frames(int pairs) { return pairs < 4 ? 8 : 4; }
 __host__ __device__ inline int64_t blocks_of(int32_t T, int32_t R) { return ((int64_t)T + R - 1) / R; }
-constexpr int kShortBlocksFrom = 512;   // tokens
+
+__host__ __device__ inline int32_t share_row(int32_t U) { return U + kShareBlanks + 1; }
 
 inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32_t U) {
     ScoreSpace s;
     const size_t hyps = (size_t)B * (size_t)N;
-    s.row = 2 * (int64_t)U + 1;
+    s.row = 2 * (int64_t)U + 2;
     const size_t off_e = align_up(hyps * sizeof(double), 256);
     const size_t off_rows = off_e + align_up(hyps * sizeof(int32_t), 256);
     const size_t places = hyps * (size_t)T * (size_t)s.row;
     const size_t off_exps = off_rows + align_up(places * sizeof(double), 256);
-    const size_t blocks = (size_t)blocks_of(T, U < kShortBlocksFrom ? 8 : 4);
+    const size_t blocks = (size_t)blocks_of(T, block_frames(lattice_pairs(B, N, U)));
     const size_t off_shares = off_exps + align_up(hyps * blocks * (size_t)s.row * sizeof(int32_t), 256);
-    s.bytes = off_shares + align_up(hyps * (size_t)T * (size_t)(U + kShareBlanks) * sizeof(float), 256);
+    s.bytes = off_shares + align_up(hyps * (size_t)T * (size_t)share_row(U) * sizeof(float), 256);
     char* p = static_cast<char*>(base);
     s.total_m = p ? reinterpret_cast<double*>(p) : nullptr;
     s.total_e = p ? reinterpret_cast<int32_t*>(p + off_e) : nullptr;

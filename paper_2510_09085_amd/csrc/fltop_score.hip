@@ -51,15 +51,20 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 // than the sum.  So a block is entered with one exponent E for each lane, no smaller than that of any
 // mass that can reach the lane within the block (those of the kReach lanes below), and if
 //   - no mass of these lanes is below 2^(E - kSpread),
-//   - no emission needed in the block is outside [kLeast, kMost], and
+//   - no emission needed in the block is outside [kLeast, kMost] (a little wider if tabulated), and
 //   - the block has all its R frames
 // then nothing leaves the range of fp64: masses stay above 2^(E - 440 - 577) and below 2^(E + 128)
 // until its end.  A frame is then three multiply-adds and two products for each pair.  Blocks that do
 // not hold this (masks of -inf, masses of e^-3000 that may be needed yet) are gone through with
 // aligned exponents.  Rows of a trained model stay within: 8 tokens at e^-25 are 288 bits.
+//
+// The exponential of an emission takes three times the frame's own work.  For vocabularies of up to
+// kTabulated tokens those of a block are taken once for all lanes, into a table in LDS, a turn ahead
+// and by all wavefronts of the direction together; for larger ones each lane takes its tokens'.
 
 constexpr int kWave = 64;
 constexpr int kSpread = 440;
+constexpr int kTabulated = 64;
 constexpr int32_t kAligned = INT32_MIN;   // in place of a lane's exponent: masses are kept as Mass32
 
 // Lane i gets lane i - 1's value, lane 0 gets `first`.
@@ -108,11 +113,19 @@ __device__ inline double exp_near(float lp) {
     return from_words((int32_t)(bits >> 32) + ((int32_t)__double_as_longlong(t) << 20), (int32_t)bits);
 }
 
+// exp(lp) of any emission: 0 or infinity where it leaves the range in which blocks are gone through with one exponent.
+__device__ inline double exp_any(float lp) {
+    const double near = exp_near(fminf(fmaxf(lp, -600.0f), 600.0f));
+    return lp < -600.0f ? 0.0 : lp <= 600.0f ? near : INFINITY;
+}
+
 // An element as it lies in memory; converted where it is used, so that loads stay in flight.
 template <int TYPE>
 __device__ inline uint32_t raw_at(const char* row, int32_t v) {
-    if constexpr (TYPE == FLTOP_TYPE_F32) return reinterpret_cast<const uint32_t*>(row)[v];
-    return reinterpret_cast<const uint16_t*>(row)[v];
+    if constexpr (TYPE == FLTOP_TYPE_F32)
+        return reinterpret_cast<const uint32_t*>(row)[v];
+    else
+        return reinterpret_cast<const uint16_t*>(row)[v];
 }
 template <int TYPE>
 __device__ inline float raw_value(uint32_t x) {
@@ -121,22 +134,62 @@ __device__ inline float raw_value(uint32_t x) {
     return __half2float(__ushort_as_half((unsigned short)x));
 }
 
+__device__ inline float value_at(const char* row, int32_t v, int32_t type) {
+    if (type == FLTOP_TYPE_F32) return raw_value<FLTOP_TYPE_F32>(raw_at<FLTOP_TYPE_F32>(row, v));
+    const uint32_t x = raw_at<FLTOP_TYPE_F16>(row, v);
+    return type == FLTOP_TYPE_BF16 ? raw_value<FLTOP_TYPE_BF16>(x) : raw_value<FLTOP_TYPE_F16>(x);
+}
+
+template <bool FIRST, typename A, typename B> struct Choose { using type = A; };
+template <typename A, typename B> struct Choose<false, A, B> { using type = B; };
+
+// An utterance's emissions.
+struct Source {
+    const char* rows;
+    int64_t frame_bytes;
+    int32_t type, V;
+};
+
 // What the wavefront above needs of a block: the last lane's token mass before each frame.  (Below the first
 // wavefront lies one without mass.)
 template <int R>
-struct Edge {
+struct alignas(8) Edge {
     double x[R];
     int32_t e[R];       // of x, if the block was gone through with aligned exponents; else E is
     int32_t E, least;   // the last lane's exponent, and the smallest that may reach it
     int32_t aligned;
 };
 
-// Edges of a workgroup: of each direction and wavefront (one below the first), for this turn and the one before.
-// Every lane writes as the last one does, the others to a place of no meaning: a store without a branch.
+// A workgroup's LDS: edges of each direction and wavefront (one below the first) for this turn and the one before;
+// a place for what is written so that the lanes that have nothing to say need no branch; tables of exponentials of
+// W + 1 blocks.  In the middle, masses of U + 1 states in place of the last two.
 template <int R>
-struct Edges {
-    Edge<R> of[2][kMostWaves + 1][2];
-    double nowhere[2 * kMostWaves][kWave + R];
+struct Lds {
+    Edge<R>* edges;      // [2][W + 1][2]
+    double* nowhere;     // [2 W][kWave + R]
+    double* tables;      // [2][W + 1][R][stride]
+    double* half_m;      // [U + 1]
+    int32_t* half_e;
+    int stride, W;
+
+    __host__ __device__ static int stride_for(int32_t V) { return V > kTabulated ? 0 : V > 32 ? 64 : 32; }
+    __device__ Lds(char* at, int waves, int32_t V, int32_t U) : stride(stride_for(V)), W(waves) {
+        edges = reinterpret_cast<Edge<R>*>(at);
+        nowhere = half_m = reinterpret_cast<double*>(edges + 4 * (W + 1));
+        tables = nowhere + 2 * W * (kWave + R);
+        half_e = reinterpret_cast<int32_t*>(half_m + U + 1);
+    }
+    static size_t bytes(int W, int32_t V, int32_t U, bool middle) {
+        const size_t way = (size_t)(2 * W * (kWave + R) + 2 * (W + 1) * R * stride_for(V)) * sizeof(double);
+        const size_t half = middle ? (size_t)(U + 1) * 12 : 0;
+        return 4 * (W + 1) * sizeof(Edge<R>) + (way > half ? way : half);
+    }
+    __device__ Edge<R>& edge(bool reversed, int wave_below, int turn) const {
+        return edges[((reversed ? W + 1 : 0) + wave_below) * 2 + (turn & 1)];
+    }
+    __device__ double* table(bool reversed, int32_t block) const {
+        return tables + ((reversed ? W + 1 : 0) + block % (W + 1)) * R * stride;
+    }
 };
 
 // What a launch does with the masses.
@@ -148,17 +201,18 @@ struct Way {
     bool reversed;
     double* rows;        // masses: written (kKeep), or the other direction's (kMeet); [T][row]
     int32_t* exps;       // their exponents, [T / R][row]
-    float* shares;       // [T][U + kShareBlanks]
+    float* shares;       // [T][share_row]
     int32_t total_e;
-    int64_t row;
+    int32_t row, share_row;
     int32_t U;
 };
 
 // The part of the lattice that one lane holds.
-template <int K, int R>
+template <int K, int R, bool TABLE>
 struct Lane {
     static constexpr int kReach = (R + K - 1) / K;   // lanes that a block's masses can come from
     static constexpr float kLeast = -400.0f / R, kMost = 80.0f / R;
+    static constexpr uint32_t kLeastWord = (1023u - 576 / R) << 20, kMostWord = (1023u + 112 / R) << 20;
 
     double xb[K], xl[K];     // masses x * 2^e
     int32_t eb[K], el[K];
@@ -166,8 +220,11 @@ struct Lane {
     double skip[K];          // 1 where y_{i+1} != y_i, else 0
     double live[K];          // 1 for pairs with a token, else 0
     int32_t i0;              // first pair
-    uint32_t raw[R][K], raw_blank;   // emissions of the next block as they lie in memory
-    float lp[R][K], lp_blank;        // those of the present one; the blank's of frame f in lane f (mod R)
+    // Emissions of the next block as they lie in memory, and those of the present one; the blank's of frame f in lane
+    // f (mod R).  With a table: what this lane adds to the next one, and its tokens' exponentials of the present block.
+    uint32_t raw[R][TABLE ? 1 : K], raw_blank;
+    using Given = typename Choose<TABLE, double, float>::type;
+    Given given[R][K], given_blank[TABLE ? R : 1];
 
     __device__ bool start(const Hyp& y, int32_t V, bool reversed, int32_t first_pair) {
         bool fine = true;
@@ -193,30 +250,30 @@ struct Lane {
 
     // Asks for the emissions of frames t0 .. t0 + nf - 1, in the order in which they are taken.
     template <int TYPE>
-    __device__ void ask_as(const char* rows, int64_t frame_bytes, int32_t t0, int32_t nf, bool reversed) {
+    __device__ void ask_as(const Source& from, int32_t t0, int32_t nf, bool reversed) {
 #pragma unroll
         for (int f = 0; f < R; ++f) {
             const int32_t g = min(f, nf - 1);
-            const char* row = rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * frame_bytes;
+            const char* row = from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes;
 #pragma unroll
-            for (int k = 0; k < K; ++k) raw[f][k] = raw_at<TYPE>(row, tok[k]);
+            for (int k = 0; k < K; ++k) raw[f][TABLE ? 0 : k] = raw_at<TYPE>(row, tok[k]);
         }
         const int32_t g = min((int32_t)(threadIdx.x & (R - 1)), nf - 1);
-        raw_blank = raw_at<TYPE>(rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * frame_bytes, 0);
+        raw_blank = raw_at<TYPE>(from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes, 0);
     }
-    __device__ void ask(const char* rows, int64_t frame_bytes, int32_t type, int32_t t0, int32_t nf, bool reversed) {
-        if (type == FLTOP_TYPE_F32)
-            ask_as<FLTOP_TYPE_F32>(rows, frame_bytes, t0, nf, reversed);
+    __device__ void ask(const Source& from, int32_t t0, int32_t nf, bool reversed) {
+        if (from.type == FLTOP_TYPE_F32)
+            ask_as<FLTOP_TYPE_F32>(from, t0, nf, reversed);
         else
-            ask_as<FLTOP_TYPE_F16>(rows, frame_bytes, t0, nf, reversed);   // 16 bits of either kind
+            ask_as<FLTOP_TYPE_F16>(from, t0, nf, reversed);   // 16 bits of either kind
     }
     template <int TYPE>
     __device__ void got_as() {
 #pragma unroll
         for (int f = 0; f < R; ++f)
 #pragma unroll
-            for (int k = 0; k < K; ++k) lp[f][k] = raw_value<TYPE>(raw[f][k]);
-        lp_blank = raw_value<TYPE>(raw_blank);
+            for (int k = 0; k < K; ++k) given[f][k] = raw_value<TYPE>(raw[f][TABLE ? 0 : k]);
+        given_blank[0] = raw_value<TYPE>(raw_blank);
     }
     __device__ void got(int32_t type) {
         if (type == FLTOP_TYPE_F32)
@@ -227,22 +284,82 @@ struct Lane {
             got_as<FLTOP_TYPE_F16>();
     }
 
+    // With a table: its rows are taken n = kWave / stride at a time, by one wavefront after the other.
+    template <int TYPE>
+    __device__ void ask_table_as(const Source& from, int stride, int wave, int W, int32_t t0, int32_t nf, bool reversed) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int n = kWave / stride;
+        const int32_t v = min((int32_t)(lane & (stride - 1)), from.V - 1);
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int f0 = (j * W + wave) * n;
+            if (f0 >= R) break;
+            const int32_t g = min(f0 + (lane >= stride ? 1 : 0), nf - 1);
+            raw[j][0] = raw_at<TYPE>(from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes, v);
+        }
+    }
+    __device__ void ask_table(const Source& from, int stride, int wave, int W, int32_t t0, int32_t nf, bool reversed) {
+        if (from.type == FLTOP_TYPE_F32)
+            ask_table_as<FLTOP_TYPE_F32>(from, stride, wave, W, t0, nf, reversed);
+        else
+            ask_table_as<FLTOP_TYPE_F16>(from, stride, wave, W, t0, nf, reversed);
+    }
+    __device__ void put_table(const Source& from, double* table, int stride, int wave, int W) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int n = kWave / stride;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int f0 = (j * W + wave) * n;
+            if (f0 >= R) break;
+            const uint32_t x = raw[j][0];
+            table[f0 * stride + lane] = exp_any(from.type == FLTOP_TYPE_F32    ? raw_value<FLTOP_TYPE_F32>(x)
+                                                : from.type == FLTOP_TYPE_BF16 ? raw_value<FLTOP_TYPE_BF16>(x)
+                                                                               : raw_value<FLTOP_TYPE_F16>(x));
+        }
+    }
+    __device__ void look_up(const double* table, int stride) {
+#pragma unroll
+        for (int f = 0; f < R; ++f) {
+            given_blank[TABLE ? f : 0] = table[f * stride];
+#pragma unroll
+            for (int k = 0; k < K; ++k) given[f][k] = table[f * stride + tok[k]];
+        }
+    }
+
     // The lane's exponent for a block, and the lane below's; returns whether the block can be gone through with them as
     // far as this lane goes.
     __device__ bool enter(const Edge<R>& in, int32_t* E, int32_t* least, int32_t* below) {
         int32_t top = kNoMass, low = -kNoMass;
-        float most = lp_blank, least_lp = lp_blank;
+        bool fine = true;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int32_t a = xb[k] == 0.0 ? kNoMass : eb[k] + __builtin_amdgcn_frexp_exp(xb[k]);
             const int32_t c = xl[k] == 0.0 ? kNoMass : el[k] + __builtin_amdgcn_frexp_exp(xl[k]);
             top = max(top, max(a, c));
             low = min(low, min(a == kNoMass ? -kNoMass : a, c == kNoMass ? -kNoMass : c));
+        }
+        if constexpr (TABLE) {
+            uint32_t most = 0, least_p = kMostWord;
 #pragma unroll
-            for (int f = 0; f < R; ++f) {
-                most = fmaxf(most, lp[f][k]);
-                least_lp = fminf(least_lp, lp[f][k]);
-            }
+            for (int f = 0; f < R; ++f)
+#pragma unroll
+                for (int k = -1; k < K; ++k) {
+                    const double one = k < 0 ? given_blank[f] : given[f][k < 0 ? 0 : k];
+                    const uint32_t w = (uint32_t)(__double_as_longlong(one) >> 32);
+                    most = max(most, w);
+                    least_p = min(least_p, w);
+                }
+            fine = least_p >= kLeastWord && most < kMostWord;
+        } else {
+            float most = given_blank[0], least_lp = given_blank[0];
+#pragma unroll
+            for (int f = 0; f < R; ++f)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    most = fmaxf(most, given[f][k]);
+                    least_lp = fminf(least_lp, given[f][k]);
+                }
+            fine = least_lp >= kLeast && most <= kMost;
         }
         int32_t m = top, n = low;
 #pragma unroll
@@ -253,7 +370,7 @@ struct Lane {
         *E = m;
         *least = n;
         *below = from_below(m, in.E);
-        return (m == kNoMass || m - n <= kSpread) && least_lp >= kLeast && most <= kMost && !in.aligned;
+        return fine && (m == kNoMass || m - n <= kSpread) && !in.aligned;
     }
 };
 
@@ -281,14 +398,26 @@ __device__ inline float sums_by_lane(float (&v)[R]) {
     return v[0];
 }
 
-// Where pair i's states are in a row: a direction's own view of the hypothesis, last pairs repeated behind the end.
-__device__ inline int32_t blank_at(const Way& way, int32_t i, int32_t L) {
-    i = min(i, L);
-    return way.reversed ? L - i : i;
-}
-__device__ inline int32_t token_at(const Way& way, int32_t i, int32_t L) {
-    i = max(min(i, L - 1), 0);
-    return way.reversed ? max(L - 1 - i, 0) : i;
+// Where a lane's states are in a row (bytes of the masses; exponents and shares have half of it): a direction's own
+// view of the hypothesis.  Lanes behind the last pair have a place of no meaning at the row's end, so that loads and
+// stores need no branch: a branch around a store would have every later wait for a load wait for the store too.
+template <int K>
+struct Places {
+    uint32_t b[K], l[K], share[K];
+    __device__ Places(const Way& way, int32_t i0, int32_t L) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int32_t i = i0 + k;
+            const int32_t bi = way.reversed ? L - i : i, li = way.reversed ? L - 1 - i : i;
+            b[k] = 8u * (uint32_t)(i <= L ? bi : way.row - 1);
+            l[k] = 8u * (uint32_t)(i < L ? way.U + 1 + li : way.row - 1);
+            share[k] = 4u * (uint32_t)(i < L ? li : way.U + kShareBlanks);
+        }
+    }
+};
+template <typename T>
+__device__ inline T& at_byte(T* base, uint32_t offset) {
+    return *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + offset);
 }
 
 // The other direction's masses of a block.
@@ -296,21 +425,21 @@ template <int K, int R>
 struct Met {
     double b[R][K], l[R][K];
     int32_t eb[K], el[K];
-    __device__ void ask(const Way& way, int32_t i0, int32_t L, int32_t t0, int32_t nf) {
-        const int32_t* exps = way.exps + (int64_t)(t0 / R) * way.row;
+    __device__ void ask(const Way& way, const Places<K>& at, int32_t t0, int32_t nf) {
+        int32_t* exps = way.exps + (int64_t)(t0 / R) * way.row;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            eb[k] = exps[blank_at(way, i0 + k, L)];
-            el[k] = exps[way.U + 1 + token_at(way, i0 + k, L)];
+            eb[k] = at_byte(exps, at.b[k] / 2);
+            el[k] = at_byte(exps, at.l[k] / 2);
         }
 #pragma unroll
         for (int f = 0; f < R; ++f) {
             const int32_t g = min(f, nf - 1);
-            const double* row = way.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - g : g)) * way.row;
+            double* row = way.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - g : g)) * way.row;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                b[f][k] = row[blank_at(way, i0 + k, L)];
-                l[f][k] = row[way.U + 1 + token_at(way, i0 + k, L)];
+                b[f][k] = at_byte(row, at.b[k]);
+                l[f][k] = at_byte(row, at.l[k]);
             }
         }
     }
@@ -336,9 +465,10 @@ __device__ inline int32_t share_shift(int32_t E, int32_t kept, int32_t total) {
 __device__ inline double share_factor(int32_t c) { return c < -1000 ? 0.0 : power_of_two(c); }
 
 // One block of frames for one wavefront.  `in`: from the wavefront below, `out`: for the one above.
-template <int K, int R, int TASK>
-__device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>& met, int32_t L, int32_t q, int wave,
-                                  const Edge<R>& in, Edge<R>& out, double* nowhere) {
+template <int K, int R, int TASK, bool TABLE>
+__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, const Met<K, R>& met, const Places<K>& at, int32_t L,
+                                  int32_t q, int wave, const Edge<R>& in, Edge<R>& out, double* nowhere,
+                                  const Source& from) {
     const int lane = threadIdx.x & (kWave - 1);
     const int32_t t0 = q * R;
     const int32_t nf = min(R, way.hi - t0);
@@ -366,8 +496,8 @@ __device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>
         int32_t* to = way.exps + (int64_t)q * way.row;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (z.i0 + k <= L) to[blank_at(way, z.i0 + k, L)] = near ? E : kAligned;
-            if (z.i0 + k < L) to[way.U + 1 + token_at(way, z.i0 + k, L)] = near ? E : kAligned;
+            at_byte(to, at.b[k] / 2) = near ? E : kAligned;
+            at_byte(to, at.l[k] / 2) = near ? E : kAligned;
         }
     }
     if (near) {
@@ -384,11 +514,16 @@ __device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>
             z.xl[k] = ldexp(z.xl[k], z.el[k] - E);
             z.eb[k] = z.el[k] = E;
         }
-        const double blank_by_lane = exp_near(z.lp_blank);
+        double blank_by_lane = 0.0;
+        if constexpr (!TABLE) blank_by_lane = exp_near(z.given_blank[0]);
 #pragma unroll
         for (int f = 0; f < R; ++f) {
             const int32_t t = t0 + (way.reversed ? R - 1 - f : f);
-            const double pb = from_lane(blank_by_lane, f);
+            double pb;
+            if constexpr (TABLE)
+                pb = z.given_blank[f];
+            else
+                pb = from_lane(blank_by_lane, f);
             edge[f] = z.xl[K - 1];
             const double moved = from_below(z.xl[K - 1], first[f]);
             double blank = 0.0;
@@ -399,16 +534,19 @@ __device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>
                 const double l = fma(prev, k > 0 ? z.skip[k] : fskip, stay);
                 const double b = k > 0 ? z.xb[k] + prev : fma(prev, fx, z.xb[k]);
                 if constexpr (TASK == kMeet) {
-                    float* to = way.shares + (int64_t)t * (way.U + kShareBlanks);
+                    // (behind the last pair there is no mass: b = 0)
                     blank += met.b[f][k] * fb[k] * b;
-                    if (z.i0 + k < L) to[token_at(way, z.i0 + k, L)] = (float)(met.l[f][k] * fl[k] * l);
+                    at_byte(way.shares + (int64_t)t * way.share_row, at.share[k]) = (float)(met.l[f][k] * fl[k] * l);
                 }
                 z.xb[k] = b * pb;
-                z.xl[k] = l * exp_near(z.lp[f][k]);
+                if constexpr (TABLE)
+                    z.xl[k] = l * z.given[f][k];
+                else
+                    z.xl[k] = l * exp_near(z.given[f][k]);
                 if constexpr (TASK == kKeep) {
                     double* to = way.rows + (int64_t)t * way.row;
-                    if (z.i0 + k <= L) to[blank_at(way, z.i0 + k, L)] = z.xb[k];
-                    if (z.i0 + k < L) to[way.U + 1 + token_at(way, z.i0 + k, L)] = z.xl[k];
+                    at_byte(to, at.b[k]) = z.xb[k];
+                    at_byte(to, at.l[k]) = z.xl[k];
                 }
             }
             blanks[f] = (float)blank;
@@ -425,20 +563,14 @@ __device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>
 #pragma unroll 1
         for (int f = 0; f < nf; ++f) {
             const int32_t t = t0 + (way.reversed ? nf - 1 - f : f);
-            const Mass blank = mass_of(__shfl(z.lp_blank, f, kWave));
+            const char* emissions = from.rows + (int64_t)t * from.frame_bytes;
+            const Mass blank = mass_of(value_at(emissions, 0, from.type));
             const Mass first = normalized(in.x[f], in.aligned ? in.e[f] : in.E);
             if (lane == kWave - 1) {
                 out.x[f] = l[K - 1].m;
                 out.e[f] = l[K - 1].e;
             }
             const Mass moved = {from_below(l[K - 1].m, first.m), from_below(l[K - 1].e, first.e)};
-            float now[K];
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                now[k] = z.lp[0][k];
-#pragma unroll
-                for (int g = 1; g < R; ++g) now[k] = g == f ? z.lp[g][k] : now[k];
-            }
             float share = 0.0f;
 #pragma unroll
             for (int k = K - 1; k >= 0; --k) {
@@ -450,24 +582,24 @@ __device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>
                 Mass on = plus(b[k], prev);
                 on = normalized(on.m, on.e);
                 if constexpr (TASK == kMeet) {
-                    const double* from = way.rows + (int64_t)t * way.row;
-                    float* to = way.shares + (int64_t)t * (way.U + kShareBlanks);
+                    double* row = way.rows + (int64_t)t * way.row;
                     if (i <= L) {
-                        const Mass m = kept_mass(from[blank_at(way, i, L)], met.eb[k]);
+                        const Mass m = kept_mass(at_byte(row, at.b[k]), met.eb[k]);
                         share += (float)ldexp(m.m * on.m, m.e + on.e - way.total_e);
                     }
                     if (i < L) {
-                        const Mass m = kept_mass(from[way.U + 1 + token_at(way, i, L)], met.el[k]);
-                        to[token_at(way, i, L)] = (float)ldexp(m.m * stay.m, m.e + stay.e - way.total_e);
+                        const Mass m = kept_mass(at_byte(row, at.l[k]), met.el[k]);
+                        at_byte(way.shares + (int64_t)t * way.share_row, at.share[k]) =
+                            (float)ldexp(m.m * stay.m, m.e + stay.e - way.total_e);
                     }
                 }
-                const Mass p = mass_of(now[k]);
+                const Mass p = mass_of(value_at(emissions, z.tok[k], from.type));
                 b[k] = normalized(on.m * blank.m, on.e + blank.e);
                 l[k] = i < L ? normalized(stay.m * p.m, stay.e + p.e) : no_mass();
                 if constexpr (TASK == kKeep) {
                     double* to = way.rows + (int64_t)t * way.row;
-                    if (i <= L) to[blank_at(way, i, L)] = keep_mass(b[k]);
-                    if (i < L) to[way.U + 1 + token_at(way, i, L)] = keep_mass(l[k]);
+                    at_byte(to, at.b[k]) = keep_mass(b[k]);
+                    at_byte(to, at.l[k]) = keep_mass(l[k]);
                 }
             }
 #pragma unroll
@@ -483,59 +615,91 @@ __device__ inline void take_block(Lane<K, R>& z, const Way& way, const Met<K, R>
     }
     if constexpr (TASK == kMeet) {
         const float sum = sums_by_lane<R>(blanks);
-        if (lane < nf) {
-            const int32_t t = t0 + (way.reversed ? nf - 1 - lane : lane);
-            way.shares[(int64_t)t * (way.U + kShareBlanks) + way.U + wave] = sum;
-        }
+        const int32_t f = min(lane, nf - 1);
+        const int32_t t = t0 + (way.reversed ? nf - 1 - f : f);
+        way.shares[(int64_t)t * way.share_row + way.U + (lane < nf ? wave : kShareBlanks)] = sum;
     }
 }
 
 // All blocks of this workgroup's two directions, a turn at a time: wavefront w of a direction is w blocks behind its
 // first.
-template <int K, int R, int TASK>
-__device__ inline void take_all(Lane<K, R>& z, const Way& way, const Way& other, int32_t L, const fltop_rows& x,
-                                int32_t b, int wave, int32_t used, Edges<R>& all) {
-    Edge<R>(*edges)[2] = all.of[way.reversed ? 1 : 0];
-    double* const nowhere = all.nowhere[(way.reversed ? kMostWaves : 0) + wave];
+template <int K, int R, int TASK, bool TABLE>
+__device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way& other, int32_t L, const Source& from,
+                                int wave, int32_t used, const Lds<R>& lds) {
+    double* const nowhere = lds.nowhere + ((way.reversed ? lds.W : 0) + wave) * (kWave + R);
     if (threadIdx.x < 4 * R) {
-        Edge<R>& none = all.of[threadIdx.x / (2 * R)][0][threadIdx.x / R & 1];
+        Edge<R>& none = lds.edge(threadIdx.x >= 2 * R, 0, threadIdx.x / R);
         none.x[threadIdx.x & (R - 1)] = 0.0;
         none.e[threadIdx.x & (R - 1)] = kNoMass;
         none.E = kNoMass;
         none.least = -kNoMass;
         none.aligned = 0;
     }
-    __syncthreads();
     const int32_t first = way.lo / R;
     const int32_t blocks = way.hi > way.lo ? (way.hi + R - 1) / R - first : 0;
     const int32_t others = other.hi > other.lo ? (other.hi + R - 1) / R - other.lo / R : 0;
     const int32_t turns = max(blocks, others) + used - 1;
-    const int32_t bytes = x.type == FLTOP_TYPE_F32 ? 4 : 2;
-    const int64_t frame_bytes = x.frame_stride * bytes;
-    const char* rows = static_cast<const char*>(x.data) + b * x.batch_stride * bytes;
-    const bool works = wave < used && blocks > 0;
-    constexpr bool kEarly = TASK == kMeet && K == 1;   // registers for two blocks of the other direction
+    constexpr bool kEarly = TASK == kMeet && K <= 2;   // registers for two blocks of the other direction
     Met<K, R> met, next;
     auto block = [&](int32_t n) { return way.reversed ? first + blocks - 1 - n : first + n; };
+    const Places<K> at(way, z.i0, L);
     auto ask = [&](int32_t n) {
-        const int32_t q = block(n), nf = min(R, way.hi - q * R);
-        z.ask(rows, frame_bytes, x.type, q * R, nf, way.reversed);
-        if constexpr (kEarly) next.ask(way, z.i0, L, q * R, nf);
+        const int32_t q = block(min(n, blocks - 1)), nf = min(R, way.hi - q * R);
+        if constexpr (!TABLE) z.ask(from, q * R, nf, way.reversed);
+        if constexpr (kEarly) next.ask(way, at, q * R, nf);
     };
-    if (works) ask(0);
-    for (int32_t turn = 0; turn < turns; ++turn) {
-        const int32_t n = turn - wave;
-        if (works && n >= 0 && n < blocks) {
-            const int32_t q = block(n);
-            z.got(x.type);
-            if constexpr (kEarly) met = next;
-            if constexpr (TASK == kMeet && !kEarly) met.ask(way, z.i0, L, q * R, min(R, way.hi - q * R));
-            if (n + 1 < blocks) ask(n + 1);
-            take_block<K, R, TASK>(z, way, met, L, q, wave, edges[wave][(turn - 1) & 1], edges[wave + 1][turn & 1],
-                                   nowhere);
+    auto ask_table = [&](int32_t n) {
+        const int32_t q = block(min(n, blocks - 1));
+        z.ask_table(from, lds.stride, wave, lds.W, q * R, min(R, way.hi - q * R), way.reversed);
+    };
+    auto put_table = [&](int32_t n) { z.put_table(from, lds.table(way.reversed, n), lds.stride, wave, lds.W); };
+    // The next block's exponentials; the block behind it is asked for.
+    auto tabulate = [&](int32_t turn) {
+        if constexpr (TABLE) {
+            if (turn + 1 < blocks) {
+                put_table(turn + 1);
+                ask_table(turn + 2);
+            }
         }
+    };
+    const bool works = wave < used && blocks > 0;
+    if (works) ask(0);
+    if constexpr (TABLE) {
+        if (blocks > 0) {
+            ask_table(0);
+            put_table(0);
+            ask_table(1);
+        }
+    }
+    __syncthreads();
+    // (three loops: with the idle turns in the loop of the blocks, a wait for a load would count on no store behind it)
+    const int32_t before = works ? wave : turns, after = works ? wave + blocks : turns;
+    for (int32_t turn = 0; turn < before; ++turn) {
+        tabulate(turn);
         __syncthreads();
     }
+    for (int32_t turn = before; turn < after; ++turn) {
+        const int32_t n = turn - wave, q = block(n);
+        tabulate(turn);
+        if constexpr (!TABLE) z.got(from.type);
+        if constexpr (kEarly) met = next;
+        if constexpr (TASK == kMeet && !kEarly) met.ask(way, at, q * R, min(R, way.hi - q * R));
+        ask(n + 1);
+        if constexpr (TABLE) z.look_up(lds.table(way.reversed, n), lds.stride);
+        take_block<K, R, TASK, TABLE>(z, way, met, at, L, q, wave, lds.edge(way.reversed, wave, turn - 1),
+                                      lds.edge(way.reversed, wave + 1, turn), nowhere, from);
+        __syncthreads();
+    }
+    for (int32_t turn = after; turn < turns; ++turn) {
+        tabulate(turn);
+        __syncthreads();
+    }
+}
+
+// The emissions of utterance b.
+__device__ inline Source source_of(const fltop_rows& x, int32_t b) {
+    const int32_t bytes = x.type == FLTOP_TYPE_F32 ? 4 : 2;
+    return {static_cast<const char*>(x.data) + b * x.batch_stride * bytes, x.frame_stride * bytes, x.type, x.V};
 }
 
 // Where the two directions of a first half meet: frames [0, middle) are the forward one's.
@@ -546,25 +710,23 @@ __host__ __device__ inline int32_t middle_of(int32_t frames) {
 }
 
 // Scores, and the lattice up to the middle from both ends.  blockDim = 2 W wavefronts.
-template <int K, int R, int THREADS, int TASK>
+template <int K, int R, int THREADS, bool TABLE, int TASK>
 __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypotheses h, double* out_scores,
                                                         ScoreSpace ws) {
     constexpr bool keep = TASK == kKeep;
-    extern __shared__ char dynamic[];   // masses of U + 1 states of the forward direction
-    __shared__ Edges<R> edges;
+    extern __shared__ char dynamic[];
     __shared__ Mass sums[2][kMostWaves];
     __shared__ Mass last[kMostWaves];
-    double* const half_m = reinterpret_cast<double*>(dynamic);
-    int32_t* const half_e = reinterpret_cast<int32_t*>(half_m + h.U + 1);
     const int64_t at = blockIdx.x;
     const int32_t b = (int32_t)(at / h.N), n = (int32_t)(at % h.N);
     const Hyp y = hypothesis(x, h, b, n);
     const int W = (int)blockDim.x / kWave / 2;
+    const Lds<R> lds(dynamic, W, x.V, h.U);
     const int lane = threadIdx.x & (kWave - 1);
     const int wave_of_all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const bool reversed = wave_of_all >= W;
     const int wave = wave_of_all - (reversed ? W : 0);
-    Lane<K, R> z;
+    Lane<K, R, TABLE> z;
     const bool fine = y.L >= 0 && z.start(y, x.V, reversed, (wave * kWave + lane) * K);
     if (__syncthreads_or(!fine)) {
         if (threadIdx.x == 0) {
@@ -577,10 +739,10 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
     const int32_t middle = middle_of<R>(y.frames);
     double* const rows = keep ? ws.rows + at * x.T * ws.row : nullptr;
     int32_t* const exps = keep ? ws.exps + at * blocks_of(x.T, R) * ws.row : nullptr;
-    const Way ways[2] = {{0, middle, false, rows, exps, nullptr, 0, ws.row, h.U},
-                         {middle, y.frames, true, rows, exps, nullptr, 0, ws.row, h.U}};
+    const Way ways[2] = {{0, middle, false, rows, exps, nullptr, 0, (int32_t)ws.row, share_row(h.U), h.U},
+                         {middle, y.frames, true, rows, exps, nullptr, 0, (int32_t)ws.row, share_row(h.U), h.U}};
     const Way way = reversed ? ways[1] : ways[0], other = reversed ? ways[0] : ways[1];
-    take_all<K, R, TASK>(z, way, other, y.L, x, b, wave, used, edges);
+    take_all<K, R, TASK, TABLE>(z, way, other, y.L, source_of(x, b), wave, used, lds);
 
     // P = sum over states of the forward mass after frame middle - 1 and the backward bracket at that frame
     if (reversed && lane == kWave - 1) last[wave] = normalized(z.xl[K - 1], z.el[K - 1]);
@@ -611,8 +773,8 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
                 const int32_t i = z.i0 + k;
                 const Mass m = part ? normalized(z.xl[k], z.el[k]) : normalized(z.xb[k], z.eb[k]);
                 if (i < y.L + 1 - part) {
-                    half_m[i] = m.m;
-                    half_e[i] = m.e;
+                    lds.half_m[i] = m.m;
+                    lds.half_e[i] = m.e;
                 }
             }
         }
@@ -625,7 +787,7 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
                 if (i >= y.L + 1 - part) continue;
                 const Mass m = part ? stay[k] : on[k];
                 const int32_t s = y.L - part - i;
-                sum = plus(sum, normalized(half_m[s] * m.m, max(half_e[s] + m.e, kNoMass)));
+                sum = plus(sum, normalized(lds.half_m[s] * m.m, max(lds.half_e[s] + m.e, kNoMass)));
                 sum = normalized(sum.m, sum.e);
             }
 #pragma unroll
@@ -649,38 +811,39 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
 }
 
 // From the middle on to both ends: occupancies, times the mantissa of P.
-template <int K, int R, int THREADS>
+template <int K, int R, int THREADS, bool TABLE>
 __global__ __launch_bounds__(THREADS) void shares_kernel(fltop_rows x, fltop_hypotheses h, ScoreSpace ws) {
-    __shared__ Edges<R> edges;
+    extern __shared__ char dynamic[];
     const int64_t at = blockIdx.x;
     const int32_t b = (int32_t)(at / h.N), n = (int32_t)(at % h.N);
     const int32_t total_e = ws.total_e[at];
     const Hyp y = hypothesis(x, h, b, n);
     if (total_e <= kNoMass || y.L < 0) return;
     const int W = (int)blockDim.x / kWave / 2;
+    const Lds<R> lds(dynamic, W, x.V, h.U);
     const int lane = threadIdx.x & (kWave - 1);
     const int wave_of_all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const bool reversed = wave_of_all >= W;
     const int wave = wave_of_all - (reversed ? W : 0);
-    Lane<K, R> z;
+    Lane<K, R, TABLE> z;
     z.start(y, x.V, reversed, (wave * kWave + lane) * K);
     const int32_t used = y.L / (kWave * K) + 1;
     const int32_t middle = middle_of<R>(y.frames);
     double* const rows = ws.rows + at * x.T * ws.row;
     int32_t* const exps = ws.exps + at * blocks_of(x.T, R) * ws.row;
-    float* const shares = ws.shares + at * x.T * (h.U + kShareBlanks);
-    const Way ways[2] = {{middle, y.frames, false, rows, exps, shares, total_e, ws.row, h.U},
-                         {0, middle, true, rows, exps, shares, total_e, ws.row, h.U}};
+    float* const shares = ws.shares + at * x.T * share_row(h.U);
+    const Way ways[2] = {{middle, y.frames, false, rows, exps, shares, total_e, (int32_t)ws.row, share_row(h.U), h.U},
+                         {0, middle, true, rows, exps, shares, total_e, (int32_t)ws.row, share_row(h.U), h.U}};
     const int32_t from = reversed ? middle : middle - 1;   // the frame that this direction went to
     if (from >= 0 && from < y.frames) {
-        const double* row = rows + from * ws.row;
-        const int32_t* e = exps + from / R * ws.row;
+        double* row = rows + from * ws.row;
+        int32_t* e = exps + from / R * ws.row;
+        const Places<K> place(ways[reversed], z.i0, y.L);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int32_t i = z.i0 + k, bs = blank_at(ways[reversed], i, y.L),
-                          ls = h.U + 1 + token_at(ways[reversed], i, y.L);
-            const Mass mb = i <= y.L ? kept_mass(row[bs], e[bs]) : no_mass();
-            const Mass ml = i < y.L ? kept_mass(row[ls], e[ls]) : no_mass();
+            const int32_t i = z.i0 + k;
+            const Mass mb = i <= y.L ? kept_mass(at_byte(row, place.b[k]), at_byte(e, place.b[k] / 2)) : no_mass();
+            const Mass ml = i < y.L ? kept_mass(at_byte(row, place.l[k]), at_byte(e, place.l[k] / 2)) : no_mass();
             z.xb[k] = mb.m;
             z.eb[k] = mb.e;
             z.xl[k] = ml.m;
@@ -688,7 +851,7 @@ __global__ __launch_bounds__(THREADS) void shares_kernel(fltop_rows x, fltop_hyp
         }
     }
     const Way way = reversed ? ways[1] : ways[0], other = reversed ? ways[0] : ways[1];
-    take_all<K, R, kMeet>(z, way, other, y.L, x, b, wave, used, edges);
+    take_all<K, R, kMeet, TABLE>(z, way, other, y.L, source_of(x, b), wave, used, lds);
 }
 
 // Occupancies into rows of V sums, which are whole numbers so that the order in which lanes add does not matter.
@@ -738,7 +901,7 @@ __global__ __launch_bounds__(kGradWaves* kWave) void score_grad_kernel(fltop_row
     wave_fence();
     constexpr double kOne = 1125899906842624.0;       // 2^50
     constexpr double kShift = 6755399441055744.0;     // 1.5 * 2^52: its last bit is worth one
-    const int64_t row = h.U + kShareBlanks;
+    const int64_t row = share_row(h.U);
     for (int32_t n = 0; n < h.N; ++n) {
         const int64_t at = (int64_t)b * h.N + n;
         if (ws.total_e[at] <= kNoMass) continue;
@@ -775,29 +938,42 @@ __global__ __launch_bounds__(kGradWaves* kWave) void score_grad_kernel(fltop_row
 }
 
 // Pairs of a lane, frames of a block, most threads.
-template <int K, int R, int THREADS>
+template <int K, int R, int THREADS, bool TABLE>
 struct Build {
-    static int waves(int32_t U) { return (U + kWave * K) / (kWave * K); }   // for U + 1 pairs
     static hipError_t score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
                             hipStream_t stream) {
-        const dim3 grid((unsigned)(x.B * h.N)), block(2 * kWave * waves(h.U));
-        const size_t lds = (size_t)(h.U + 1) * 12;
+        const int W = waves_for(h.U, K);
+        const dim3 grid((unsigned)(x.B * h.N)), block(2 * kWave * W);
+        const size_t bytes = Lds<R>::bytes(W, x.V, h.U, true);
         if (keep)
-            hipLaunchKernelGGL((score_kernel<K, R, THREADS, kKeep>), grid, block, lds, stream, x, h, out_scores, *keep);
+            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, kKeep>), grid, block, bytes, stream, x, h, out_scores,
+                               *keep);
         else
-            hipLaunchKernelGGL((score_kernel<K, R, THREADS, kScore>), grid, block, lds, stream, x, h, out_scores,
+            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, kScore>), grid, block, bytes, stream, x, h, out_scores,
                                ScoreSpace{});
         return hipGetLastError();
     }
     static hipError_t shares(const fltop_rows& x, const fltop_hypotheses& h, const ScoreSpace& ws, hipStream_t stream) {
-        hipLaunchKernelGGL((shares_kernel<K, R, THREADS>), dim3((unsigned)(x.B * h.N)), dim3(2 * kWave * waves(h.U)), 0,
-                           stream, x, h, ws);
+        const int W = waves_for(h.U, K);
+        hipLaunchKernelGGL((shares_kernel<K, R, THREADS, TABLE>), dim3((unsigned)(x.B * h.N)), dim3(2 * kWave * W),
+                           Lds<R>::bytes(W, x.V, h.U, false), stream, x, h, ws);
         return hipGetLastError();
     }
 };
 
-// Pairs that a lane holds: as few as keep a direction within four wavefronts (up to 2047 tokens; eight beyond).
-int pairs_per_lane(int32_t U) { return U < 256 ? 1 : U < kShortBlocksFrom ? 2 : U < 1024 ? 4 : 8; }
+// Calls `f` with the build for these shapes.
+template <typename F>
+hipError_t with_build(const fltop_rows& x, const fltop_hypotheses& h, F f) {
+    const bool table = x.V <= kTabulated;
+    switch (lattice_pairs(x.B, h.N, h.U)) {
+        case 1: return table ? f(Build<1, 8, 256, true>{}) : f(Build<1, 8, 256, false>{});
+        case 2: return table ? f(Build<2, 8, 256, true>{}) : f(Build<2, 8, 256, false>{});
+        case 4: return table ? f(Build<4, 4, 256, true>{}) : f(Build<4, 4, 256, false>{});
+        default:
+            if (waves_for(h.U, 8) <= 2) return table ? f(Build<8, 4, 256, true>{}) : f(Build<8, 4, 256, false>{});
+            return table ? f(Build<8, 4, 1024, true>{}) : f(Build<8, 4, 1024, false>{});
+    }
+}
 
 template <typename T>
 hipError_t grad_of(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores, const ScoreSpace& ws,
@@ -810,7 +986,7 @@ hipError_t grad_of(const fltop_rows& x, const fltop_hypotheses& h, const double*
     const int64_t blocks = ((int64_t)x.B * chunks + waves - 1) / waves;
     hipLaunchKernelGGL(score_grad_kernel<T>, dim3((unsigned)blocks), dim3(waves * kWave),
                        (size_t)waves * per_wave * x.V * sizeof(unsigned long long), stream, x, h, grad_scores, ws,
-                       per_wave, chunks, kWave * pairs_per_lane(h.U), static_cast<T*>(grad));
+                       per_wave, chunks, kWave * lattice_pairs(x.B, h.N, h.U), static_cast<T*>(grad));
     return hipGetLastError();
 }
 
@@ -818,23 +994,12 @@ hipError_t grad_of(const fltop_rows& x, const fltop_hypotheses& h, const double*
 
 hipError_t launch_score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
                         hipStream_t stream) {
-    switch (pairs_per_lane(h.U)) {
-        case 1: return Build<1, 8, 512>::score(x, h, out_scores, keep, stream);
-        case 2: return Build<2, 8, 512>::score(x, h, out_scores, keep, stream);
-        case 4: return Build<4, 4, 512>::score(x, h, out_scores, keep, stream);
-        default: return Build<8, 4, 1024>::score(x, h, out_scores, keep, stream);
-    }
+    return with_build(x, h, [&](auto build) { return decltype(build)::score(x, h, out_scores, keep, stream); });
 }
 
 hipError_t launch_score_grad(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores,
                              const ScoreSpace& ws, void* grad, hipStream_t stream) {
-    hipError_t e;
-    switch (pairs_per_lane(h.U)) {
-        case 1: e = Build<1, 8, 512>::shares(x, h, ws, stream); break;
-        case 2: e = Build<2, 8, 512>::shares(x, h, ws, stream); break;
-        case 4: e = Build<4, 4, 512>::shares(x, h, ws, stream); break;
-        default: e = Build<8, 4, 1024>::shares(x, h, ws, stream); break;
-    }
+    const hipError_t e = with_build(x, h, [&](auto build) { return decltype(build)::shares(x, h, ws, stream); });
     if (e != hipSuccess) return e;
     if (x.type == FLTOP_TYPE_BF16) return grad_of<__hip_bfloat16>(x, h, grad_scores, ws, grad, stream);
     if (x.type == FLTOP_TYPE_F16) return grad_of<__half>(x, h, grad_scores, ws, grad, stream);
