@@ -326,13 +326,14 @@ typedef struct fltop_hypotheses {
  * apart, so that it neither under- nor overflows.  -inf: the hypothesis has no alignment -- too
  * few frames, only impossible ones, or a token that is the blank or not below V.  Hypotheses at
  * or beyond counts[b] and those of negative length are not there: their score is -inf too.  A
- * hypothesis of more than U tokens is not scored: NaN.  An emission below -7e8 counts as -inf;
- * NaN and +inf are undefined, as in the decoder.
+ * hypothesis of more than U tokens is not scored: NaN.  An emission (or an
+ * alignment) below -7e8 counts as -inf; NaN and +inf are undefined, as in the decoder.
  *   workspace  NULL if only the scores are wanted; else dev, 256-byte aligned, of at least
  *              fltop_ctc_score_workspace_bytes(B, T, N, U) bytes, into which the call puts what
  *              fltop_ctc_score_grad goes on from.
- * Refused: B, T, N < 1, V < 2, U < 1 or beyond FLTOP_MAX_LABELS, B * N >= 2^31 (BAD_SHAPE), V >
- * FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type (BAD_OPTION). */
+ * Refused: B, T, N < 1, V < 2, U < 1 or beyond FLTOP_MAX_LABELS, B * N or B * T >= 2^31
+ * (BAD_SHAPE), N > FLTOP_MAX_BEAM (BAD_BEAM), V > FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type
+ * (BAD_OPTION). */
 size_t fltop_ctc_score_workspace_bytes(int32_t B, int32_t T, int32_t N, int32_t U);
 int fltop_ctc_score(const fltop_rows* logprobs, const fltop_hypotheses* hyps, double* out_scores,
                     void* workspace, size_t workspace_bytes, void* hip_stream);

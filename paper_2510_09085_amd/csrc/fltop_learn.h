@@ -74,18 +74,16 @@ __device__ inline Mass plus(Mass a, Mass b) {
     return {ldexp(a.m, a.e - e) + ldexp(b.m, b.e - e), e};  // not normalized
 }
 
-constexpr int kMostWaves = 8;             // wavefronts that one direction of a lattice takes
-constexpr int kShareBlanks = kMostWaves;  // places for the blanks' occupancy behind a frame's tokens
+constexpr int kMostWaves = 8;   // wavefronts that one direction of a lattice takes
 
-// What fltop_ctc_score leaves for fltop_ctc_score_grad.  The states of a hypothesis of L tokens are
-// its L + 1 blanks (places 0..L of a row) and its tokens (from place U + 1 on).
+// What fltop_ctc_score leaves for fltop_ctc_score_grad.
 struct ScoreSpace {
     double* total_m;   // [B*N] P(hypothesis) as a Mass; kNoMass for one that takes no part
     int32_t* total_e;  // [B*N]
-    double* rows;      // [B*N][T][row] masses of the alignments up to a state, without their exponents
-    int32_t* exps;     // [B*N][blocks of frames][row] those exponents
-    float* shares;     // [B*N][T][share_row] occupancies of the tokens, then of all blanks in parts
-    int64_t row;       // 2U + 1, and a place for what has no meaning
+    double* marks;     // [B*N][2][blocks][row] masses of both directions at the borders of blocks of frames
+    int32_t* mark_exps;   // their exponents, alike
+    int64_t row;       // 2U + 1 states and a place for what has no meaning
+    int64_t marks_of;  // places of one direction of one hypothesis
     size_t bytes;
 };
 
@@ -93,32 +91,28 @@ struct ScoreSpace {
 // workgroup's wavefronts has a SIMD for itself (eight of eight pairs beyond 1023 tokens).
 inline int lattice_pairs(int32_t B, int32_t N, int32_t U) {
     (void)B, (void)N;
-    return U < 128 ? 1 : U < 256 ? 2 : U < 512 ? 4 : 8;
+    return U < 256 ? 2 : U < 512 ? 4 : 8;
 }
 inline int waves_for(int32_t U, int pairs) { return (U + 64 * pairs) / (64 * pairs); }   // for U + 1 pairs
 // Frames that are gone through together: exponents are kept once for each such block.
 inline int block_frames(int pairs) { return pairs < 4 ? 8 : 4; }
 __host__ __device__ inline int64_t blocks_of(int32_t T, int32_t R) { return ((int64_t)T + R - 1) / R; }
 
-__host__ __device__ inline int32_t share_row(int32_t U) { return U + kShareBlanks + 1; }
-
 inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32_t U) {
     ScoreSpace s;
     const size_t hyps = (size_t)B * (size_t)N;
     s.row = 2 * (int64_t)U + 2;
+    s.marks_of = blocks_of(T, block_frames(lattice_pairs(B, N, U))) * s.row;
     const size_t off_e = align_up(hyps * sizeof(double), 256);
-    const size_t off_rows = off_e + align_up(hyps * sizeof(int32_t), 256);
-    const size_t places = hyps * (size_t)T * (size_t)s.row;
-    const size_t off_exps = off_rows + align_up(places * sizeof(double), 256);
-    const size_t blocks = (size_t)blocks_of(T, block_frames(lattice_pairs(B, N, U)));
-    const size_t off_shares = off_exps + align_up(hyps * blocks * (size_t)s.row * sizeof(int32_t), 256);
-    s.bytes = off_shares + align_up(hyps * (size_t)T * (size_t)share_row(U) * sizeof(float), 256);
+    const size_t off_marks = off_e + align_up(hyps * sizeof(int32_t), 256);
+    const size_t places = hyps * 2 * (size_t)s.marks_of;
+    const size_t off_exps = off_marks + align_up(places * sizeof(double), 256);
+    s.bytes = off_exps + align_up(places * sizeof(int32_t), 256);
     char* p = static_cast<char*>(base);
     s.total_m = p ? reinterpret_cast<double*>(p) : nullptr;
     s.total_e = p ? reinterpret_cast<int32_t*>(p + off_e) : nullptr;
-    s.rows = p ? reinterpret_cast<double*>(p + off_rows) : nullptr;
-    s.exps = p ? reinterpret_cast<int32_t*>(p + off_exps) : nullptr;
-    s.shares = p ? reinterpret_cast<float*>(p + off_shares) : nullptr;
+    s.marks = p ? reinterpret_cast<double*>(p + off_marks) : nullptr;
+    s.mark_exps = p ? reinterpret_cast<int32_t*>(p + off_exps) : nullptr;
     return s;
 }
 

@@ -18,16 +18,17 @@ int check_rows(const fltop_rows* x, bool decodes) {
 }
 
 bool lattice_shapes(int32_t B, int32_t T, int32_t N, int32_t U) {
-    return B >= 1 && T >= 1 && N >= 1 && U >= 1 && U <= FLTOP_MAX_LABELS && (int64_t)B * N <= (int64_t)INT32_MAX;
+    return B >= 1 && T >= 1 && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 && U <= FLTOP_MAX_LABELS && (int64_t)B * N <= (int64_t)INT32_MAX;
 }
 
 // Whether the lattices of these shapes can be addressed (their places as bytes within 63 bits).
 bool lattice_fits(int32_t B, int32_t T, int32_t N, int32_t U) {
-    return lattice_shapes(B, T, N, U) && (double)B * N * T * (2.0 * U + 1.0) < 7e16;
+    return lattice_shapes(B, T, N, U) && (double)B * N * T * (2.0 * U + 1100.0) < 7e16;
 }
 
 int check_hypotheses(const fltop_rows* x, const fltop_hypotheses* h) {
     if (!h || !h->tokens || !h->lengths) return FLTOP_ERR_NULL_POINTER;
+    if (h->N > FLTOP_MAX_BEAM) return FLTOP_ERR_BAD_BEAM;
     if (!lattice_shapes(x->B, x->T, h->N, h->U)) return FLTOP_ERR_BAD_SHAPE;
     if (h->token_batch_stride < 0 || h->token_stride < 0 || h->length_batch_stride < 0) return FLTOP_ERR_BAD_SHAPE;
     return FLTOP_OK;

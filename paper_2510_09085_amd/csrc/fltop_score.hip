@@ -38,10 +38,11 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 // ---- how a hypothesis is laid out over the lanes -------------------------------------------------
 //
 // A workgroup takes one hypothesis, forwards and backwards at once: W wavefronts for each direction,
-// lane by lane K pairs (b_i, l_i) each.  Both directions go to the middle of the utterance (the
-// score is there), and with a gradient wanted a second kernel goes on from the middle to the two
-// ends, each direction past the masses that the other has left: half as many serial frames as one
-// direction after the other.
+// lane by lane K pairs (b_i, l_i) each.  For the score alone both directions go to the middle of the
+// utterance: half as many serial frames as one direction would have.  With a gradient wanted both go
+// all the way and leave their masses at the borders of the blocks (below); a second kernel then goes
+// through the blocks of all utterances at once, once more from either border, and needs no masses of
+// single frames in memory.
 //
 // Frames come in blocks of R.  Within a block only l_{i-1} passes from lane to lane (one DPP shift),
 // and the wavefront above takes the same block one turn later with the last lane's masses from LDS,
@@ -51,21 +52,19 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 // than the sum.  So a block is entered with one exponent E for each lane, no smaller than that of any
 // mass that can reach the lane within the block (those of the kReach lanes below), and if
 //   - no mass of these lanes is below 2^(E - kSpread),
-//   - no emission needed in the block is outside [kLeast, kMost] (a little wider if tabulated), and
+//   - no emission needed in the block is below 2^-58 (e^-40) or from 2^14 up, and
 //   - the block has all its R frames
-// then nothing leaves the range of fp64: masses stay above 2^(E - 440 - 577) and below 2^(E + 128)
+// then nothing leaves the range of fp64: masses stay above 2^(E - kSpread - 58 R) and below 2^(E + 128)
 // until its end.  A frame is then three multiply-adds and two products for each pair.  Blocks that do
 // not hold this (masks of -inf, masses of e^-3000 that may be needed yet) are gone through with
-// aligned exponents.  Rows of a trained model stay within: 8 tokens at e^-25 are 288 bits.
+// aligned exponents.  Rows of a trained model stay within: 10 tokens at e^-25 are 360 bits.
 //
 // The exponential of an emission takes three times the frame's own work.  For vocabularies of up to
-// kTabulated tokens those of a block are taken once for all lanes, into a table in LDS, a turn ahead
-// and by all wavefronts of the direction together; for larger ones each lane takes its tokens'.
+// kTabulated tokens a wavefront more for each direction takes all of a block's, a turn ahead, into a
+// table in LDS; for larger ones each lane takes its tokens'.
 
 constexpr int kWave = 64;
-constexpr int kSpread = 440;
 constexpr int kTabulated = 64;
-constexpr int32_t kAligned = INT32_MIN;   // in place of a lane's exponent: masses are kept as Mass32
 
 // Lane i gets lane i - 1's value, lane 0 gets `first`.
 __device__ inline int32_t from_below(int32_t x, int32_t first) {
@@ -86,8 +85,15 @@ __device__ inline double from_lane(double x, int lane) {
 
 // 2^e for e in [-1022, 1023].
 __device__ inline double power_of_two(int32_t e) { return from_words((e + 1023) << 20, 0); }
+// 2^e as a factor of masses of which those that leave the range are 0.
+__device__ inline double rescaling(int32_t e) { return power_of_two(max(min(e, 1000), -1022)); }
+__device__ inline uint32_t high_word(double x) { return (uint32_t)(__double_as_longlong(x) >> 32); }
 
-// exp(lp) for lp in [kLeast, kMost], as mass_of, with k taken from the last bits of a number in which they are worth
+// Emissions that a block may have to be gone through with one exponent for each lane.
+constexpr float kLeastNear = -40.0f, kMostNear = 9.7f;
+constexpr uint32_t kLeastWord = (1023u - 58) << 20, kMostWord = (1023u + 14) << 20;
+
+// exp(lp) for lp within +-600, as mass_of, with k taken from the last bits of a number in which they are worth
 // one and added to the result's exponent.
 __device__ inline double exp_near(float lp) {
     const double x = lp;
@@ -127,17 +133,13 @@ __device__ inline uint32_t raw_at(const char* row, int32_t v) {
     else
         return reinterpret_cast<const uint16_t*>(row)[v];
 }
-template <int TYPE>
-__device__ inline float raw_value(uint32_t x) {
-    if constexpr (TYPE == FLTOP_TYPE_F32) return __uint_as_float(x);
-    if constexpr (TYPE == FLTOP_TYPE_BF16) return __uint_as_float(x << 16);
-    return __half2float(__ushort_as_half((unsigned short)x));
+__device__ inline float raw_value(uint32_t x, int32_t type) {
+    const float half = __half2float(__ushort_as_half((unsigned short)x));
+    return type == FLTOP_TYPE_F32 ? __uint_as_float(x) : type == FLTOP_TYPE_BF16 ? __uint_as_float(x << 16) : half;
 }
 
 __device__ inline float value_at(const char* row, int32_t v, int32_t type) {
-    if (type == FLTOP_TYPE_F32) return raw_value<FLTOP_TYPE_F32>(raw_at<FLTOP_TYPE_F32>(row, v));
-    const uint32_t x = raw_at<FLTOP_TYPE_F16>(row, v);
-    return type == FLTOP_TYPE_BF16 ? raw_value<FLTOP_TYPE_BF16>(x) : raw_value<FLTOP_TYPE_F16>(x);
+    return raw_value(type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, v) : raw_at<FLTOP_TYPE_F16>(row, v), type);
 }
 
 template <bool FIRST, typename A, typename B> struct Choose { using type = A; };
@@ -162,73 +164,79 @@ struct alignas(8) Edge {
 
 // A workgroup's LDS: edges of each direction and wavefront (one below the first) for this turn and the one before;
 // a place for what is written so that the lanes that have nothing to say need no branch; tables of exponentials of
-// W + 1 blocks.  In the middle, masses of U + 1 states in place of the last two.
-template <int R>
+// W + 1 blocks, and whether one of them is out of range.  In the middle, masses of U + 1 states in place of the last two.
+template <int R, bool TABLE>
 struct Lds {
     Edge<R>* edges;      // [2][W + 1][2]
+    int32_t* wide;       // [2][W + 1]
     double* nowhere;     // [2 W][kWave + R]
-    double* tables;      // [2][W + 1][R][stride]
+    double* tables;      // [2][W + 1][R][kTabulated]
     double* half_m;      // [U + 1]
     int32_t* half_e;
-    int stride, W;
+    int W;
 
-    __host__ __device__ static int stride_for(int32_t V) { return V > kTabulated ? 0 : V > 32 ? 64 : 32; }
-    __device__ Lds(char* at, int waves, int32_t V, int32_t U) : stride(stride_for(V)), W(waves) {
+    __device__ Lds(char* at, int waves, int32_t U) : W(waves) {
         edges = reinterpret_cast<Edge<R>*>(at);
-        nowhere = half_m = reinterpret_cast<double*>(edges + 4 * (W + 1));
+        wide = reinterpret_cast<int32_t*>(edges + 4 * (W + 1));
+        nowhere = half_m = reinterpret_cast<double*>(wide + 2 * (W + 1));
         tables = nowhere + 2 * W * (kWave + R);
         half_e = reinterpret_cast<int32_t*>(half_m + U + 1);
     }
-    static size_t bytes(int W, int32_t V, int32_t U, bool middle) {
-        const size_t way = (size_t)(2 * W * (kWave + R) + 2 * (W + 1) * R * stride_for(V)) * sizeof(double);
-        const size_t half = middle ? (size_t)(U + 1) * 12 : 0;
-        return 4 * (W + 1) * sizeof(Edge<R>) + (way > half ? way : half);
+    static size_t bytes(int W, int32_t U, bool middle) {
+        const size_t tables = TABLE ? 2 * (W + 1) * R * kTabulated : 0;
+        const size_t way = (2 * W * (kWave + R) + tables) * sizeof(double), half = middle ? (size_t)(U + 1) * 12 : 0;
+        return 4 * (W + 1) * sizeof(Edge<R>) + 2 * (W + 1) * sizeof(int32_t) + (way > half ? way : half);
     }
     __device__ Edge<R>& edge(bool reversed, int wave_below, int turn) const {
         return edges[((reversed ? W + 1 : 0) + wave_below) * 2 + (turn & 1)];
     }
-    __device__ double* table(bool reversed, int32_t block) const {
-        return tables + ((reversed ? W + 1 : 0) + block % (W + 1)) * R * stride;
-    }
+    __device__ int slot(bool reversed, int32_t block) const { return (reversed ? W + 1 : 0) + block % (W + 1); }
+    __device__ double* table(int slot) const { return tables + slot * (R * kTabulated); }
 };
-
-// What a launch does with the masses.
-constexpr int kScore = 0, kKeep = 1, kMeet = 2;
 
 // What a direction does in a launch.
 struct Way {
     int32_t lo, hi;      // its frames
     bool reversed;
-    double* rows;        // masses: written (kKeep), or the other direction's (kMeet); [T][row]
-    int32_t* exps;       // their exponents, [T / R][row]
-    float* shares;       // [T][share_row]
-    int32_t total_e;
-    int32_t row, share_row;
+    double* marks;       // masses at the borders of blocks, [blocks][row] (or NULL)
+    int32_t* mark_exps;  // their exponents, alike
+    int32_t row;
     int32_t U;
 };
+
+// Where pair i's states are in a row of border masses: blanks, then tokens, then a place of no meaning for lanes behind
+// the last pair, so that a store needs no branch.
+__device__ inline int32_t blank_place(const Way& way, int32_t i, int32_t L) {
+    return i > L ? way.row - 1 : way.reversed ? L - i : i;
+}
+__device__ inline int32_t token_place(const Way& way, int32_t i, int32_t L) {
+    return i >= L ? way.row - 1 : way.U + 1 + (way.reversed ? L - 1 - i : i);
+}
 
 // The part of the lattice that one lane holds.
 template <int K, int R, bool TABLE>
 struct Lane {
     static constexpr int kReach = (R + K - 1) / K;   // lanes that a block's masses can come from
-    static constexpr float kLeast = -400.0f / R, kMost = 80.0f / R;
-    static constexpr uint32_t kLeastWord = (1023u - 576 / R) << 20, kMostWord = (1023u + 112 / R) << 20;
+    static constexpr int kSpread = 1017 - 58 * R;
 
-    double xb[K], xl[K];     // masses x * 2^e
-    int32_t eb[K], el[K];
+    double xb[K], xl[K];     // masses x * 2^E, or x * 2^eb and x * 2^el if not `common`
+    int32_t E, eb[K], el[K];
+    bool common;             // (alike in all lanes)
     int32_t tok[K];          // 0 behind the last token
     double skip[K];          // 1 where y_{i+1} != y_i, else 0
     double live[K];          // 1 for pairs with a token, else 0
     int32_t i0;              // first pair
-    // Emissions of the next block as they lie in memory, and those of the present one; the blank's of frame f in lane
-    // f (mod R).  With a table: what this lane adds to the next one, and its tokens' exponentials of the present block.
-    uint32_t raw[R][TABLE ? 1 : K], raw_blank;
+    // Without a table: emissions of the next block as they lie in memory, those of the present one, the blank's of frame f
+    // in lane f (mod R).  With one: the exponentials of the present block.
+    uint32_t raw[TABLE ? 1 : R][K], raw_blank;
     using Given = typename Choose<TABLE, double, float>::type;
     Given given[R][K], given_blank[TABLE ? R : 1];
 
     __device__ bool start(const Hyp& y, int32_t V, bool reversed, int32_t first_pair) {
         bool fine = true;
         i0 = first_pair;
+        E = 0;
+        common = true;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int32_t i = i0 + k;
@@ -241,12 +249,13 @@ struct Lane {
                 tok[k] = 0;
             }
             xb[k] = i == 0 ? 1.0 : 0.0;
-            eb[k] = i == 0 ? 0 : kNoMass;
             xl[k] = 0.0;
-            el[k] = kNoMass;
+            eb[k] = el[k] = 0;
         }
         return fine;
     }
+    __device__ Mass blank_mass(int k) const { return normalized(xb[k], common ? E : eb[k]); }
+    __device__ Mass token_mass(int k) const { return normalized(xl[k], common ? E : el[k]); }
 
     // Asks for the emissions of frames t0 .. t0 + nf - 1, in the order in which they are taken.
     template <int TYPE>
@@ -256,7 +265,7 @@ struct Lane {
             const int32_t g = min(f, nf - 1);
             const char* row = from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes;
 #pragma unroll
-            for (int k = 0; k < K; ++k) raw[f][TABLE ? 0 : k] = raw_at<TYPE>(row, tok[k]);
+            for (int k = 0; k < K; ++k) raw[TABLE ? 0 : f][k] = raw_at<TYPE>(row, tok[k]);
         }
         const int32_t g = min((int32_t)(threadIdx.x & (R - 1)), nf - 1);
         raw_blank = raw_at<TYPE>(from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes, 0);
@@ -267,99 +276,72 @@ struct Lane {
         else
             ask_as<FLTOP_TYPE_F16>(from, t0, nf, reversed);   // 16 bits of either kind
     }
-    template <int TYPE>
-    __device__ void got_as() {
+    __device__ void got(int32_t type) {
 #pragma unroll
         for (int f = 0; f < R; ++f)
 #pragma unroll
-            for (int k = 0; k < K; ++k) given[f][k] = raw_value<TYPE>(raw[f][TABLE ? 0 : k]);
-        given_blank[0] = raw_value<TYPE>(raw_blank);
+            for (int k = 0; k < K; ++k) given[f][k] = raw_value(raw[TABLE ? 0 : f][k], type);
+        given_blank[0] = raw_value(raw_blank, type);
     }
-    __device__ void got(int32_t type) {
-        if (type == FLTOP_TYPE_F32)
-            got_as<FLTOP_TYPE_F32>();
-        else if (type == FLTOP_TYPE_BF16)
-            got_as<FLTOP_TYPE_BF16>();
-        else
-            got_as<FLTOP_TYPE_F16>();
-    }
-
-    // With a table: its rows are taken n = kWave / stride at a time, by one wavefront after the other.
-    template <int TYPE>
-    __device__ void ask_table_as(const Source& from, int stride, int wave, int W, int32_t t0, int32_t nf, bool reversed) {
-        const int lane = threadIdx.x & (kWave - 1);
-        const int n = kWave / stride;
-        const int32_t v = min((int32_t)(lane & (stride - 1)), from.V - 1);
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int f0 = (j * W + wave) * n;
-            if (f0 >= R) break;
-            const int32_t g = min(f0 + (lane >= stride ? 1 : 0), nf - 1);
-            raw[j][0] = raw_at<TYPE>(from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes, v);
-        }
-    }
-    __device__ void ask_table(const Source& from, int stride, int wave, int W, int32_t t0, int32_t nf, bool reversed) {
-        if (from.type == FLTOP_TYPE_F32)
-            ask_table_as<FLTOP_TYPE_F32>(from, stride, wave, W, t0, nf, reversed);
-        else
-            ask_table_as<FLTOP_TYPE_F16>(from, stride, wave, W, t0, nf, reversed);
-    }
-    __device__ void put_table(const Source& from, double* table, int stride, int wave, int W) {
-        const int lane = threadIdx.x & (kWave - 1);
-        const int n = kWave / stride;
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int f0 = (j * W + wave) * n;
-            if (f0 >= R) break;
-            const uint32_t x = raw[j][0];
-            table[f0 * stride + lane] = exp_any(from.type == FLTOP_TYPE_F32    ? raw_value<FLTOP_TYPE_F32>(x)
-                                                : from.type == FLTOP_TYPE_BF16 ? raw_value<FLTOP_TYPE_BF16>(x)
-                                                                               : raw_value<FLTOP_TYPE_F16>(x));
-        }
-    }
-    __device__ void look_up(const double* table, int stride) {
+    __device__ void look_up(const double* table) {
 #pragma unroll
         for (int f = 0; f < R; ++f) {
-            given_blank[TABLE ? f : 0] = table[f * stride];
+            given_blank[TABLE ? f : 0] = table[f * kTabulated];
 #pragma unroll
-            for (int k = 0; k < K; ++k) given[f][k] = table[f * stride + tok[k]];
+            for (int k = 0; k < K; ++k) given[f][k] = table[f * kTabulated + tok[k]];
         }
     }
 
-    // The lane's exponent for a block, and the lane below's; returns whether the block can be gone through with them as
-    // far as this lane goes.
-    __device__ bool enter(const Edge<R>& in, int32_t* E, int32_t* least, int32_t* below) {
-        int32_t top = kNoMass, low = -kNoMass;
-        bool fine = true;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int32_t a = xb[k] == 0.0 ? kNoMass : eb[k] + __builtin_amdgcn_frexp_exp(xb[k]);
-            const int32_t c = xl[k] == 0.0 ? kNoMass : el[k] + __builtin_amdgcn_frexp_exp(xl[k]);
-            top = max(top, max(a, c));
-            low = min(low, min(a == kNoMass ? -kNoMass : a, c == kNoMass ? -kNoMass : c));
-        }
+    // Whether this lane's emissions of the block are in range.
+    __device__ bool in_range() const {
         if constexpr (TABLE) {
-            uint32_t most = 0, least_p = kMostWord;
+            uint32_t most = 0, least = kMostWord;
 #pragma unroll
             for (int f = 0; f < R; ++f)
 #pragma unroll
                 for (int k = -1; k < K; ++k) {
-                    const double one = k < 0 ? given_blank[f] : given[f][k < 0 ? 0 : k];
-                    const uint32_t w = (uint32_t)(__double_as_longlong(one) >> 32);
+                    const uint32_t w = high_word(k < 0 ? given_blank[f] : given[f][k < 0 ? 0 : k]);
                     most = max(most, w);
-                    least_p = min(least_p, w);
+                    least = min(least, w);
                 }
-            fine = least_p >= kLeastWord && most < kMostWord;
+            return least >= kLeastWord && most < kMostWord;
         } else {
-            float most = given_blank[0], least_lp = given_blank[0];
+            float most = given_blank[0], least = given_blank[0];
 #pragma unroll
             for (int f = 0; f < R; ++f)
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     most = fmaxf(most, given[f][k]);
-                    least_lp = fminf(least_lp, given[f][k]);
+                    least = fminf(least, given[f][k]);
                 }
-            fine = least_lp >= kLeast && most <= kMost;
+            return least >= kLeastNear && most <= kMostNear;
+        }
+    }
+
+    // The lane's exponent for a block, the smallest that may reach it, and the lane below's; returns whether the spread
+    // is within bounds.
+    __device__ bool enter(const Edge<R>& in, int32_t* to, int32_t* least, int32_t* below) const {
+        int32_t top = kNoMass, low = -kNoMass;
+        if (common) {
+            uint32_t most = 0, few = UINT32_MAX;   // high words; less one, so that 0 is none
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const uint32_t a = high_word(xb[k]), c = high_word(xl[k]);
+                most = max(most, max(a, c));
+                few = min(few, min(a - 1, c - 1));
+            }
+            if (most != 0) {
+                top = E + (int32_t)(most >> 20) - 1022;
+                low = E + (int32_t)(few >> 20) - 1022;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int32_t a = xb[k] == 0.0 ? kNoMass : eb[k] + __builtin_amdgcn_frexp_exp(xb[k]);
+                const int32_t c = xl[k] == 0.0 ? kNoMass : el[k] + __builtin_amdgcn_frexp_exp(xl[k]);
+                top = max(top, max(a, c));
+                low = min(low, min(a == kNoMass ? -kNoMass : a, c == kNoMass ? -kNoMass : c));
+            }
         }
         int32_t m = top, n = low;
 #pragma unroll
@@ -367,17 +349,37 @@ struct Lane {
             m = max(from_below(m, in.E), top);
             n = min(from_below(n, in.least), low);
         }
-        *E = m;
+        *to = m;
         *least = n;
         *below = from_below(m, in.E);
-        return fine && (m == kNoMass || m - n <= kSpread) && !in.aligned;
+        return m == kNoMass || m - n <= kSpread;
+    }
+
+    // Masses with the lane's new exponent.
+    __device__ void rescale(int32_t to) {
+        if (common) {
+            const double by = rescaling(E - to);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                xb[k] *= by;
+                xl[k] *= by;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                xb[k] = ldexp(xb[k], eb[k] - to);
+                xl[k] = ldexp(xl[k], el[k] - to);
+            }
+        }
+        E = to;
+        common = true;
     }
 };
 
 // Sums of v[0..R) over the wavefront, in a fixed order; lane f (mod R) returns that of v[f].  Each of the
 // first steps halves the number of values that a lane carries.
 template <int R>
-__device__ inline float sums_by_lane(float (&v)[R]) {
+__device__ inline double sums_by_lane(double (&v)[R]) {
     const int lane = threadIdx.x & (kWave - 1);
     int n = R;
 #pragma unroll
@@ -388,8 +390,8 @@ __device__ inline float sums_by_lane(float (&v)[R]) {
         for (int j = 0; j < R / 2; ++j) {
             if (j >= n) break;
             // lanes without bit o keep the even places, lanes with it the odd ones
-            const float keep = upper ? v[2 * j + 1] : v[2 * j];
-            const float give = upper ? v[2 * j] : v[2 * j + 1];
+            const double keep = upper ? v[2 * j + 1] : v[2 * j];
+            const double give = upper ? v[2 * j] : v[2 * j + 1];
             v[j] = keep + __shfl_xor(give, o, kWave);
         }
     }
@@ -398,127 +400,47 @@ __device__ inline float sums_by_lane(float (&v)[R]) {
     return v[0];
 }
 
-// Where a lane's states are in a row (bytes of the masses; exponents and shares have half of it): a direction's own
-// view of the hypothesis.  Lanes behind the last pair have a place of no meaning at the row's end, so that loads and
-// stores need no branch: a branch around a store would have every later wait for a load wait for the store too.
-template <int K>
-struct Places {
-    uint32_t b[K], l[K], share[K];
-    __device__ Places(const Way& way, int32_t i0, int32_t L) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int32_t i = i0 + k;
-            const int32_t bi = way.reversed ? L - i : i, li = way.reversed ? L - 1 - i : i;
-            b[k] = 8u * (uint32_t)(i <= L ? bi : way.row - 1);
-            l[k] = 8u * (uint32_t)(i < L ? way.U + 1 + li : way.row - 1);
-            share[k] = 4u * (uint32_t)(i < L ? li : way.U + kShareBlanks);
-        }
-    }
-};
-template <typename T>
-__device__ inline T& at_byte(T* base, uint32_t offset) {
-    return *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + offset);
-}
-
-// The other direction's masses of a block.
-template <int K, int R>
-struct Met {
-    double b[R][K], l[R][K];
-    int32_t eb[K], el[K];
-    __device__ void ask(const Way& way, const Places<K>& at, int32_t t0, int32_t nf) {
-        int32_t* exps = way.exps + (int64_t)(t0 / R) * way.row;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            eb[k] = at_byte(exps, at.b[k] / 2);
-            el[k] = at_byte(exps, at.l[k] / 2);
-        }
-#pragma unroll
-        for (int f = 0; f < R; ++f) {
-            const int32_t g = min(f, nf - 1);
-            double* row = way.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - g : g)) * way.row;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                b[f][k] = at_byte(row, at.b[k]);
-                l[f][k] = at_byte(row, at.l[k]);
-            }
-        }
-    }
-};
-
-// A kept mass with its exponent e, whichever way it was kept.
-__device__ inline Mass kept_mass(double x, int32_t e) {
-    if (e != kAligned) return normalized(x, e);
-    const long long bits = __double_as_longlong(x);
-    return {__uint_as_float((uint32_t)bits), (int32_t)(bits >> 32)};
-}
-__device__ inline double keep_mass(Mass x) { return from_words(x.e, (int32_t)__float_as_uint((float)x.m)); }
-
-// The product of two masses becomes a share by 2^c, with c their exponents less that of P.  Masses are below 2^128, so
-// that a share of weight has c > -300; up to kMostShift one mass times 2^c stays in range whatever the other is.
-constexpr int32_t kMostShift = 880;
-__device__ inline int32_t share_shift(int32_t E, int32_t kept, int32_t total) {
-    if (kept == kAligned) return kMostShift + 1;
-    if (kept <= kNoMass || E <= kNoMass) return -2000;
-    const long long c = (long long)E + kept - total;
-    return (int32_t)(c < -2000 ? -2000 : c > kMostShift ? kMostShift + 1 : c);
-}
-__device__ inline double share_factor(int32_t c) { return c < -1000 ? 0.0 : power_of_two(c); }
-
 // One block of frames for one wavefront.  `in`: from the wavefront below, `out`: for the one above.
-template <int K, int R, int TASK, bool TABLE>
-__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, const Met<K, R>& met, const Places<K>& at, int32_t L,
-                                  int32_t q, int wave, const Edge<R>& in, Edge<R>& out, double* nowhere,
-                                  const Source& from) {
+template <int K, int R, bool TABLE>
+__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t L, int32_t q, bool wide, const Edge<R>& in,
+                                  Edge<R>& out, double* nowhere, const Source& from) {
     const int lane = threadIdx.x & (kWave - 1);
     const int32_t t0 = q * R;
     const int32_t nf = min(R, way.hi - t0);
-    float blanks[R];
-    int32_t E, least, below;
-    bool fine = z.enter(in, &E, &least, &below) && nf == R;
-    double fb[K], fl[K];
-    if constexpr (TASK == kMeet) {
+    if (way.marks) {
+        double* const m = way.marks + (int64_t)q * way.row;
+        int32_t* const e = way.mark_exps + (int64_t)q * way.row;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int32_t cb = share_shift(E, met.eb[k], way.total_e), cl = share_shift(E, met.el[k], way.total_e);
-            fine &= z.i0 + k > L || cb <= kMostShift;
-            fine &= z.i0 + k >= L || cl <= kMostShift;
-            fb[k] = share_factor(min(cb, kMostShift));
-            fl[k] = share_factor(min(cl, kMostShift));
+            const int32_t bp = blank_place(way, z.i0 + k, L), lp = token_place(way, z.i0 + k, L);
+            m[bp] = z.xb[k];
+            e[bp] = z.common ? z.E : z.eb[k];
+            m[lp] = z.xl[k];
+            e[lp] = z.common ? z.E : z.el[k];
         }
     }
+    int32_t E, least, below;
+    bool fine = z.enter(in, &E, &least, &below) && nf == R && !in.aligned;
+    if (!TABLE || wide) fine &= z.in_range();
     const bool near = __all(fine);
     if (lane == kWave - 1) {
         out.E = E;
         out.least = least;
         out.aligned = !near;
     }
-    if constexpr (TASK == kKeep) {
-        int32_t* to = way.exps + (int64_t)q * way.row;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            at_byte(to, at.b[k] / 2) = near ? E : kAligned;
-            at_byte(to, at.l[k] / 2) = near ? E : kAligned;
-        }
-    }
     if (near) {
         // the lane below's scale in this one's
-        const double fx = ldexp(1.0, min(below - E, 1000));
+        const double fx = rescaling(below - E);
         const double fskip = fx * z.skip[0];
         double* const edge = lane == kWave - 1 ? out.x : nowhere + lane;
         double first[R];
 #pragma unroll
         for (int f = 0; f < R; ++f) first[f] = in.x[f];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            z.xb[k] = ldexp(z.xb[k], z.eb[k] - E);
-            z.xl[k] = ldexp(z.xl[k], z.el[k] - E);
-            z.eb[k] = z.el[k] = E;
-        }
+        z.rescale(E);
         double blank_by_lane = 0.0;
         if constexpr (!TABLE) blank_by_lane = exp_near(z.given_blank[0]);
 #pragma unroll
         for (int f = 0; f < R; ++f) {
-            const int32_t t = t0 + (way.reversed ? R - 1 - f : f);
             double pb;
             if constexpr (TABLE)
                 pb = z.given_blank[f];
@@ -526,44 +448,30 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, const Me
                 pb = from_lane(blank_by_lane, f);
             edge[f] = z.xl[K - 1];
             const double moved = from_below(z.xl[K - 1], first[f]);
-            double blank = 0.0;
 #pragma unroll
             for (int k = K - 1; k >= 0; --k) {
                 const double prev = k > 0 ? z.xl[k > 0 ? k - 1 : 0] : moved;
                 const double stay = fma(z.xb[k], z.live[k], z.xl[k]);
                 const double l = fma(prev, k > 0 ? z.skip[k] : fskip, stay);
                 const double b = k > 0 ? z.xb[k] + prev : fma(prev, fx, z.xb[k]);
-                if constexpr (TASK == kMeet) {
-                    // (behind the last pair there is no mass: b = 0)
-                    blank += met.b[f][k] * fb[k] * b;
-                    at_byte(way.shares + (int64_t)t * way.share_row, at.share[k]) = (float)(met.l[f][k] * fl[k] * l);
-                }
                 z.xb[k] = b * pb;
                 if constexpr (TABLE)
                     z.xl[k] = l * z.given[f][k];
                 else
                     z.xl[k] = l * exp_near(z.given[f][k]);
-                if constexpr (TASK == kKeep) {
-                    double* to = way.rows + (int64_t)t * way.row;
-                    at_byte(to, at.b[k]) = z.xb[k];
-                    at_byte(to, at.l[k]) = z.xl[k];
-                }
             }
-            blanks[f] = (float)blank;
         }
     } else {
         Mass b[K], l[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            b[k] = normalized(z.xb[k], z.eb[k]);
-            l[k] = normalized(z.xl[k], z.el[k]);
+            b[k] = z.blank_mass(k);
+            l[k] = z.token_mass(k);
         }
-#pragma unroll
-        for (int f = 0; f < R; ++f) blanks[f] = 0.0f;
+        z.common = false;
 #pragma unroll 1
         for (int f = 0; f < nf; ++f) {
-            const int32_t t = t0 + (way.reversed ? nf - 1 - f : f);
-            const char* emissions = from.rows + (int64_t)t * from.frame_bytes;
+            const char* emissions = from.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - f : f)) * from.frame_bytes;
             const Mass blank = mass_of(value_at(emissions, 0, from.type));
             const Mass first = normalized(in.x[f], in.aligned ? in.e[f] : in.E);
             if (lane == kWave - 1) {
@@ -571,39 +479,16 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, const Me
                 out.e[f] = l[K - 1].e;
             }
             const Mass moved = {from_below(l[K - 1].m, first.m), from_below(l[K - 1].e, first.e)};
-            float share = 0.0f;
 #pragma unroll
             for (int k = K - 1; k >= 0; --k) {
-                const int32_t i = z.i0 + k;
                 const Mass prev = k > 0 ? l[k > 0 ? k - 1 : 0] : moved;
                 Mass stay = plus(l[k], b[k]);
                 if (z.skip[k] != 0.0) stay = plus(stay, prev);
-                stay = normalized(stay.m, stay.e);
-                Mass on = plus(b[k], prev);
-                on = normalized(on.m, on.e);
-                if constexpr (TASK == kMeet) {
-                    double* row = way.rows + (int64_t)t * way.row;
-                    if (i <= L) {
-                        const Mass m = kept_mass(at_byte(row, at.b[k]), met.eb[k]);
-                        share += (float)ldexp(m.m * on.m, m.e + on.e - way.total_e);
-                    }
-                    if (i < L) {
-                        const Mass m = kept_mass(at_byte(row, at.l[k]), met.el[k]);
-                        at_byte(way.shares + (int64_t)t * way.share_row, at.share[k]) =
-                            (float)ldexp(m.m * stay.m, m.e + stay.e - way.total_e);
-                    }
-                }
+                const Mass on = plus(b[k], prev);
                 const Mass p = mass_of(value_at(emissions, z.tok[k], from.type));
                 b[k] = normalized(on.m * blank.m, on.e + blank.e);
-                l[k] = i < L ? normalized(stay.m * p.m, stay.e + p.e) : no_mass();
-                if constexpr (TASK == kKeep) {
-                    double* to = way.rows + (int64_t)t * way.row;
-                    at_byte(to, at.b[k]) = keep_mass(b[k]);
-                    at_byte(to, at.l[k]) = keep_mass(l[k]);
-                }
+                l[k] = z.live[k] != 0.0 ? normalized(stay.m * p.m, stay.e + p.e) : no_mass();
             }
-#pragma unroll
-            for (int g = 0; g < R; ++g) blanks[g] = g == f ? share : blanks[g];
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -613,87 +498,132 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, const Me
             z.el[k] = l[k].e;
         }
     }
-    if constexpr (TASK == kMeet) {
-        const float sum = sums_by_lane<R>(blanks);
-        const int32_t f = min(lane, nf - 1);
-        const int32_t t = t0 + (way.reversed ? nf - 1 - f : f);
-        way.shares[(int64_t)t * way.share_row + way.U + (lane < nf ? wave : kShareBlanks)] = sum;
+}
+
+// The blocks of a direction in the order in which it takes them, and the turns of the workgroup: wavefront w is w
+// blocks behind its direction's first.
+template <int R>
+struct Blocks {
+    int32_t first, count, turns;
+    bool reversed;
+    __device__ Blocks(const Way& way, const Way& other, int32_t used) : first(way.lo / R), reversed(way.reversed) {
+        count = way.hi > way.lo ? (way.hi + R - 1) / R - first : 0;
+        const int32_t others = other.hi > other.lo ? (other.hi + R - 1) / R - other.lo / R : 0;
+        turns = max(count, others) + used - 1;
+    }
+    // (the last one again behind the end)
+    __device__ int32_t operator[](int32_t n) const {
+        n = min(n, count - 1);
+        return reversed ? first + count - 1 - n : first + n;
+    }
+};
+
+// The wavefront that tabulates: block n + 1 in turn n, asked for two turns before.
+template <int R>
+struct Tabulator {
+    uint32_t raw[R];
+    template <int TYPE>
+    __device__ void ask_as(const Source& from, const Way& way, int32_t q) {
+        const int32_t v = min((int32_t)(threadIdx.x & (kWave - 1)), from.V - 1);
+        const int32_t nf = min(R, way.hi - q * R);
+#pragma unroll
+        for (int f = 0; f < R; ++f) {
+            const int32_t g = min(f, nf - 1);
+            raw[f] = raw_at<TYPE>(from.rows + (int64_t)(q * R + (way.reversed ? nf - 1 - g : g)) * from.frame_bytes, v);
+        }
+    }
+    __device__ void ask(const Source& from, const Way& way, int32_t q) {
+        if (from.type == FLTOP_TYPE_F32)
+            ask_as<FLTOP_TYPE_F32>(from, way, q);
+        else
+            ask_as<FLTOP_TYPE_F16>(from, way, q);
+    }
+    __device__ void put(const Source& from, double* table, int32_t* wide) {
+        const int lane = threadIdx.x & (kWave - 1);
+        bool near = true;
+#pragma unroll
+        for (int f = 0; f < R; ++f) {
+            const float lp = raw_value(raw[f], from.type);
+            near &= lp >= kLeastNear && lp <= kMostNear;
+            table[f * kTabulated + lane] = exp_any(lp);
+        }
+        const bool all = __all(near);
+        if (lane == 0) *wide = !all;
+    }
+};
+
+template <int R>
+__device__ inline void tabulate_all(const Way& way, const Way& other, const Source& from, int32_t used,
+                                    const Lds<R, true>& lds) {
+    const Blocks<R> blocks(way, other, used);
+    Tabulator<R> even, odd;
+    auto put = [&](Tabulator<R>& one, int32_t n) {
+        const int slot = lds.slot(way.reversed, n);
+        one.put(from, lds.table(slot), lds.wide + slot);
+    };
+    if (blocks.count > 0) {
+        even.ask(from, way, blocks[0]);
+        odd.ask(from, way, blocks[1]);
+        put(even, 0);
+        even.ask(from, way, blocks[2]);
+    }
+    __syncthreads();
+    for (int32_t turn = 0; turn < blocks.turns; turn += 2) {
+        if (turn + 1 < blocks.count) {
+            put(odd, turn + 1);
+            odd.ask(from, way, blocks[turn + 3]);
+        }
+        __syncthreads();
+        if (turn + 1 >= blocks.turns) break;
+        if (turn + 2 < blocks.count) {
+            put(even, turn + 2);
+            even.ask(from, way, blocks[turn + 4]);
+        }
+        __syncthreads();
     }
 }
 
-// All blocks of this workgroup's two directions, a turn at a time: wavefront w of a direction is w blocks behind its
-// first.
-template <int K, int R, int TASK, bool TABLE>
+// A wavefront's blocks.
+template <int K, int R, bool TABLE>
 __device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way& other, int32_t L, const Source& from,
-                                int wave, int32_t used, const Lds<R>& lds) {
+                                int wave, int32_t used, const Lds<R, TABLE>& lds) {
     double* const nowhere = lds.nowhere + ((way.reversed ? lds.W : 0) + wave) * (kWave + R);
-    if (threadIdx.x < 4 * R) {
-        Edge<R>& none = lds.edge(threadIdx.x >= 2 * R, 0, threadIdx.x / R);
-        none.x[threadIdx.x & (R - 1)] = 0.0;
-        none.e[threadIdx.x & (R - 1)] = kNoMass;
+    if (wave == 0 && threadIdx.x % kWave < 2 * R) {   // nothing comes from below the first
+        const int32_t f = threadIdx.x & (R - 1);
+        Edge<R>& none = lds.edge(way.reversed, 0, threadIdx.x % kWave / R);
+        none.x[f] = 0.0;
+        none.e[f] = kNoMass;
         none.E = kNoMass;
         none.least = -kNoMass;
         none.aligned = 0;
     }
-    const int32_t first = way.lo / R;
-    const int32_t blocks = way.hi > way.lo ? (way.hi + R - 1) / R - first : 0;
-    const int32_t others = other.hi > other.lo ? (other.hi + R - 1) / R - other.lo / R : 0;
-    const int32_t turns = max(blocks, others) + used - 1;
-    constexpr bool kEarly = TASK == kMeet && K <= 2;   // registers for two blocks of the other direction
-    Met<K, R> met, next;
-    auto block = [&](int32_t n) { return way.reversed ? first + blocks - 1 - n : first + n; };
-    const Places<K> at(way, z.i0, L);
+    const Blocks<R> blocks(way, other, used);
     auto ask = [&](int32_t n) {
-        const int32_t q = block(min(n, blocks - 1)), nf = min(R, way.hi - q * R);
-        if constexpr (!TABLE) z.ask(from, q * R, nf, way.reversed);
-        if constexpr (kEarly) next.ask(way, at, q * R, nf);
+        const int32_t q = blocks[n];
+        if constexpr (!TABLE) z.ask(from, q * R, min(R, way.hi - q * R), way.reversed);
     };
-    auto ask_table = [&](int32_t n) {
-        const int32_t q = block(min(n, blocks - 1));
-        z.ask_table(from, lds.stride, wave, lds.W, q * R, min(R, way.hi - q * R), way.reversed);
-    };
-    auto put_table = [&](int32_t n) { z.put_table(from, lds.table(way.reversed, n), lds.stride, wave, lds.W); };
-    // The next block's exponentials; the block behind it is asked for.
-    auto tabulate = [&](int32_t turn) {
-        if constexpr (TABLE) {
-            if (turn + 1 < blocks) {
-                put_table(turn + 1);
-                ask_table(turn + 2);
-            }
-        }
-    };
-    const bool works = wave < used && blocks > 0;
+    const bool works = wave < used && blocks.count > 0;
     if (works) ask(0);
-    if constexpr (TABLE) {
-        if (blocks > 0) {
-            ask_table(0);
-            put_table(0);
-            ask_table(1);
-        }
-    }
     __syncthreads();
     // (three loops: with the idle turns in the loop of the blocks, a wait for a load would count on no store behind it)
-    const int32_t before = works ? wave : turns, after = works ? wave + blocks : turns;
-    for (int32_t turn = 0; turn < before; ++turn) {
-        tabulate(turn);
-        __syncthreads();
-    }
+    const int32_t before = works ? wave : blocks.turns, after = works ? wave + blocks.count : blocks.turns;
+    for (int32_t turn = 0; turn < before; ++turn) __syncthreads();
     for (int32_t turn = before; turn < after; ++turn) {
-        const int32_t n = turn - wave, q = block(n);
-        tabulate(turn);
-        if constexpr (!TABLE) z.got(from.type);
-        if constexpr (kEarly) met = next;
-        if constexpr (TASK == kMeet && !kEarly) met.ask(way, at, q * R, min(R, way.hi - q * R));
-        ask(n + 1);
-        if constexpr (TABLE) z.look_up(lds.table(way.reversed, n), lds.stride);
-        take_block<K, R, TASK, TABLE>(z, way, met, at, L, q, wave, lds.edge(way.reversed, wave, turn - 1),
-                                      lds.edge(way.reversed, wave + 1, turn), nowhere, from);
+        const int32_t n = turn - wave;
+        bool wide = true;
+        if constexpr (TABLE) {
+            const int slot = lds.slot(way.reversed, n);
+            wide = __builtin_amdgcn_readfirstlane(lds.wide[slot]);
+            z.look_up(lds.table(slot));
+        } else {
+            z.got(from.type);
+            ask(n + 1);
+        }
+        take_block<K, R, TABLE>(z, way, L, blocks[n], wide, lds.edge(way.reversed, wave, turn - 1),
+                                lds.edge(way.reversed, wave + 1, turn), nowhere, from);
         __syncthreads();
     }
-    for (int32_t turn = after; turn < turns; ++turn) {
-        tabulate(turn);
-        __syncthreads();
-    }
+    for (int32_t turn = after; turn < blocks.turns; ++turn) __syncthreads();
 }
 
 // The emissions of utterance b.
@@ -709,69 +639,111 @@ __host__ __device__ inline int32_t middle_of(int32_t frames) {
     return h < frames ? h : frames;
 }
 
-// Scores, and the lattice up to the middle from both ends.  blockDim = 2 W wavefronts.
-template <int K, int R, int THREADS, bool TABLE, int TASK>
+// A wavefront's part in its workgroup: W wavefronts of one direction, then one that tabulates for it, then the other's.
+template <int K, bool TABLE>
+struct Role {
+    int W, wave, lane;
+    bool reversed, tabulates;
+    __device__ Role() {
+        const int n = (int)blockDim.x / kWave / 2;   // of a direction
+        const int all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+        W = TABLE ? n - 1 : n;
+        reversed = all >= n;
+        wave = all - (reversed ? n : 0);
+        tabulates = TABLE && wave == W;
+        lane = threadIdx.x & (kWave - 1);
+    }
+    __device__ int32_t first_pair() const { return (wave * kWave + lane) * K; }
+};
+
+// Scores; with KEEP also the masses at the borders of blocks, of both directions.
+template <int K, int R, int THREADS, bool TABLE, bool KEEP>
 __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypotheses h, double* out_scores,
                                                         ScoreSpace ws) {
-    constexpr bool keep = TASK == kKeep;
     extern __shared__ char dynamic[];
-    __shared__ Mass sums[2][kMostWaves];
+    __shared__ Mass sums[kMostWaves];
     __shared__ Mass last[kMostWaves];
     const int64_t at = blockIdx.x;
     const int32_t b = (int32_t)(at / h.N), n = (int32_t)(at % h.N);
     const Hyp y = hypothesis(x, h, b, n);
-    const int W = (int)blockDim.x / kWave / 2;
-    const Lds<R> lds(dynamic, W, x.V, h.U);
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave_of_all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const bool reversed = wave_of_all >= W;
-    const int wave = wave_of_all - (reversed ? W : 0);
+    const Role<K, TABLE> role;
+    const Lds<R, TABLE> lds(dynamic, role.W, h.U);
+    const bool reversed = role.reversed;
     Lane<K, R, TABLE> z;
-    const bool fine = y.L >= 0 && z.start(y, x.V, reversed, (wave * kWave + lane) * K);
+    // (the lanes of a wavefront that tabulates lie behind the last pair)
+    const bool fine = y.L >= 0 && z.start(y, x.V, reversed, role.tabulates ? y.L + 1 : role.first_pair());
     if (__syncthreads_or(!fine)) {
         if (threadIdx.x == 0) {
             out_scores[at] = y.L == -2 ? NAN : -INFINITY;
-            if (keep) ws.total_m[at] = 0.0, ws.total_e[at] = kNoMass;
+            if (KEEP) ws.total_m[at] = 0.0, ws.total_e[at] = kNoMass;
         }
         return;
     }
     const int32_t used = y.L / (kWave * K) + 1;
-    const int32_t middle = middle_of<R>(y.frames);
-    double* const rows = keep ? ws.rows + at * x.T * ws.row : nullptr;
-    int32_t* const exps = keep ? ws.exps + at * blocks_of(x.T, R) * ws.row : nullptr;
-    const Way ways[2] = {{0, middle, false, rows, exps, nullptr, 0, (int32_t)ws.row, share_row(h.U), h.U},
-                         {middle, y.frames, true, rows, exps, nullptr, 0, (int32_t)ws.row, share_row(h.U), h.U}};
-    const Way way = reversed ? ways[1] : ways[0], other = reversed ? ways[0] : ways[1];
-    take_all<K, R, TASK, TABLE>(z, way, other, y.L, source_of(x, b), wave, used, lds);
+    const int32_t middle = KEEP ? y.frames : middle_of<R>(y.frames);
+    Way forward = {0, middle, false, nullptr, nullptr, (int32_t)ws.row, h.U};
+    Way backward = {KEEP ? 0 : middle, y.frames, true, nullptr, nullptr, (int32_t)ws.row, h.U};
+    if constexpr (KEEP) {
+        forward.marks = ws.marks + at * 2 * ws.marks_of;
+        forward.mark_exps = ws.mark_exps + at * 2 * ws.marks_of;
+        backward.marks = forward.marks + ws.marks_of;
+        backward.mark_exps = forward.mark_exps + ws.marks_of;
+    }
+    const Way way = reversed ? backward : forward, other = reversed ? forward : backward;
+    if (role.tabulates) {
+        if constexpr (TABLE) tabulate_all<R>(way, other, source_of(x, b), used, lds);
+    } else {
+        take_all<K, R, TABLE>(z, way, other, y.L, source_of(x, b), role.wave, used, lds);
+    }
+    if constexpr (KEEP) {
+        // P = b_L + l_{L-1} after the last frame
+        if (!reversed && !role.tabulates) {
+            Mass end = no_mass();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (z.i0 + k == y.L) end = plus(end, z.blank_mass(k));
+                if (z.i0 + k == y.L - 1) end = plus(end, z.token_mass(k));
+                end = normalized(end.m, end.e);
+            }
+            if (z.i0 <= y.L && y.L < z.i0 + K) sums[0] = end;
+            if (z.i0 <= y.L - 1 && y.L - 1 < z.i0 + K && !(z.i0 <= y.L && y.L < z.i0 + K)) sums[1] = end;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            // (both states may be one lane's)
+            Mass p = y.L % K != 0 || y.L == 0 ? sums[0] : plus(sums[0], sums[1]);
+            p = normalized(p.m, p.e);
+            out_scores[at] = ln_of(p);
+            ws.total_m[at] = p.m;
+            ws.total_e[at] = p.e;
+        }
+        return;
+    }
 
     // P = sum over states of the forward mass after frame middle - 1 and the backward bracket at that frame
-    if (reversed && lane == kWave - 1) last[wave] = normalized(z.xl[K - 1], z.el[K - 1]);
+    const bool back = reversed && !role.tabulates, fore = !reversed && !role.tabulates;
+    if (back && role.lane == kWave - 1) last[role.wave] = z.token_mass(K - 1);
     __syncthreads();
-    Mass on[K], stay[K];
-    if (reversed) {
-        Mass l[K], bl[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            l[k] = normalized(z.xl[k], z.el[k]);
-            bl[k] = normalized(z.xb[k], z.eb[k]);
-        }
-        const Mass first = wave > 0 ? last[wave > 0 ? wave - 1 : 0] : no_mass();
-        const Mass moved = {from_below(l[K - 1].m, first.m), from_below(l[K - 1].e, first.e)};
+    Mass on[K], stay[K], sum = no_mass();
+    if (back) {
+        const Mass first = role.wave > 0 ? last[role.wave - 1] : no_mass();
+        const Mass top = z.token_mass(K - 1);
+        const Mass moved = {from_below(top.m, first.m), from_below(top.e, first.e)};
 #pragma unroll
         for (int k = K - 1; k >= 0; --k) {
-            const Mass prev = k > 0 ? l[k > 0 ? k - 1 : 0] : moved;
-            stay[k] = plus(l[k], bl[k]);
+            const Mass prev = k > 0 ? z.token_mass(k > 0 ? k - 1 : 0) : moved, blank = z.blank_mass(k);
+            stay[k] = plus(z.token_mass(k), blank);
             if (z.skip[k] != 0.0) stay[k] = plus(stay[k], prev);
-            on[k] = plus(bl[k], prev);
+            on[k] = plus(blank, prev);
         }
     }
 #pragma unroll
     for (int part = 0; part < 2; ++part) {   // blanks, then tokens
-        if (!reversed && wave < used) {
+        if (fore) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int32_t i = z.i0 + k;
-                const Mass m = part ? normalized(z.xl[k], z.el[k]) : normalized(z.xb[k], z.eb[k]);
+                const Mass m = part ? z.token_mass(k) : z.blank_mass(k);
                 if (i < y.L + 1 - part) {
                     lds.half_m[i] = m.m;
                     lds.half_e[i] = m.e;
@@ -779,8 +751,7 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
             }
         }
         __syncthreads();
-        if (reversed) {
-            Mass sum = no_mass();
+        if (back) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int32_t i = z.i0 + k;
@@ -788,175 +759,375 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
                 const Mass m = part ? stay[k] : on[k];
                 const int32_t s = y.L - part - i;
                 sum = plus(sum, normalized(lds.half_m[s] * m.m, max(lds.half_e[s] + m.e, kNoMass)));
-                sum = normalized(sum.m, sum.e);
             }
-#pragma unroll
-            for (int o = kWave / 2; o > 0; o >>= 1) {
-                sum = plus(sum, {__shfl_xor(sum.m, o, kWave), __shfl_xor(sum.e, o, kWave)});
-                sum = normalized(sum.m, sum.e);
-            }
-            if (lane == 0) sums[part][wave] = sum;
         }
         __syncthreads();
     }
+    if (back) {
+        int32_t e = sum.e;
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) e = max(e, __shfl_xor(e, o, kWave));
+        double m = ldexp(sum.m, sum.e - e);
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) m += __shfl_xor(m, o, kWave);
+        if (role.lane == 0) sums[role.wave] = normalized(m, e);
+    }
+    __syncthreads();
     if (threadIdx.x == 0) {
         Mass p = no_mass();
-        for (int w = 0; w < W; ++w) {
-            p = plus(p, plus(sums[0][w], sums[1][w]));
+        for (int w = 0; w < role.W; ++w) {
+            p = plus(p, sums[w]);
             p = normalized(p.m, p.e);
         }
         out_scores[at] = ln_of(p);
-        if (keep) ws.total_m[at] = p.m, ws.total_e[at] = p.e;
     }
 }
 
-// From the middle on to both ends: occupancies, times the mantissa of P.
-template <int K, int R, int THREADS, bool TABLE>
-__global__ __launch_bounds__(THREADS) void shares_kernel(fltop_rows x, fltop_hypotheses h, ScoreSpace ws) {
-    extern __shared__ char dynamic[];
-    const int64_t at = blockIdx.x;
-    const int32_t b = (int32_t)(at / h.N), n = (int32_t)(at % h.N);
-    const int32_t total_e = ws.total_e[at];
-    const Hyp y = hypothesis(x, h, b, n);
-    if (total_e <= kNoMass || y.L < 0) return;
-    const int W = (int)blockDim.x / kWave / 2;
-    const Lds<R> lds(dynamic, W, x.V, h.U);
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave_of_all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const bool reversed = wave_of_all >= W;
-    const int wave = wave_of_all - (reversed ? W : 0);
-    Lane<K, R, TABLE> z;
-    z.start(y, x.V, reversed, (wave * kWave + lane) * K);
-    const int32_t used = y.L / (kWave * K) + 1;
-    const int32_t middle = middle_of<R>(y.frames);
-    double* const rows = ws.rows + at * x.T * ws.row;
-    int32_t* const exps = ws.exps + at * blocks_of(x.T, R) * ws.row;
-    float* const shares = ws.shares + at * x.T * share_row(h.U);
-    const Way ways[2] = {{middle, y.frames, false, rows, exps, shares, total_e, (int32_t)ws.row, share_row(h.U), h.U},
-                         {0, middle, true, rows, exps, shares, total_e, (int32_t)ws.row, share_row(h.U), h.U}};
-    const int32_t from = reversed ? middle : middle - 1;   // the frame that this direction went to
-    if (from >= 0 && from < y.frames) {
-        double* row = rows + from * ws.row;
-        int32_t* e = exps + from / R * ws.row;
-        const Places<K> place(ways[reversed], z.i0, y.L);
+// ---- the gradient -----------------------------------------------------------------------------------
+//
+// A workgroup takes one block of R frames of an utterance, and its wavefronts that block's hypotheses, each in chunks
+// of kWave K pairs: forwards from the masses at the block's lower border, with the masses after each frame in registers;
+// then backwards from those at the upper border, both in the same lanes.  Within a block a mass goes R pairs far, so
+// chunks that overlap by 2 R pairs need nothing from each other.  Occupancies are added to rows of V sums in LDS, as
+// whole numbers: in any order the same.  The conditions for one exponent for each lane are those of the scores'
+// blocks, for both directions, and that P's exponent is within reach of theirs.
+
+constexpr int kGradPairs = 2, kGradThreads = 256;
+
+__device__ inline int32_t from_above(int32_t x, int32_t last) {
+    return __builtin_amdgcn_update_dpp(last, x, 0x130, 0xf, 0xf, false);  // wave_shl:1
+}
+__device__ inline double from_above(double x) {
+    const long long a = __double_as_longlong(x);
+    return from_words(from_above((int32_t)(a >> 32), 0), from_above((int32_t)a, 0));
+}
+
+// 2^c by which the product of two masses of exponents that add up to c becomes an occupancy, less that of P.  Masses are
+// below 2^128, so that an occupancy of weight has c > -300; up to kMostShift one mass times 2^c stays in range whatever
+// the other is.
+constexpr int32_t kMostShift = 880;
+__device__ inline int32_t share_shift(int32_t Ef, int32_t Eb, int32_t total) {
+    if (Ef <= kNoMass || Eb <= kNoMass) return -2000;
+    const long long c = (long long)Ef + Eb - total;
+    return (int32_t)(c < -2000 ? -2000 : c > kMostShift ? kMostShift + 1 : c);
+}
+
+// A lane's pairs of one chunk.
+template <int K, int R>
+struct Chunk {
+    int32_t tok[K], i0, L;
+    double skip[K], skip_up[K], live[K];   // skip_up: of the pair above
+    Mass fb[K], fl[K], bb[K], bl[K];       // masses at the lower border (forwards) and the upper one (backwards)
+
+    __device__ Chunk(const Hyp& y, const ScoreSpace& ws, int64_t at, int32_t U, int32_t V, int32_t q, int32_t first_pair)
+        : i0(first_pair + (int32_t)(threadIdx.x & (kWave - 1)) * K), L(y.L) {
+        const Way up = {0, 0, false, nullptr, nullptr, (int32_t)ws.row, U};
+        const double* fm = ws.marks + at * 2 * ws.marks_of + q * ws.row;
+        const int32_t* fe = ws.mark_exps + at * 2 * ws.marks_of + q * ws.row;
+        const double* bm = fm + ws.marks_of;
+        const int32_t* be = fe + ws.marks_of;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int32_t i = z.i0 + k;
-            const Mass mb = i <= y.L ? kept_mass(at_byte(row, place.b[k]), at_byte(e, place.b[k] / 2)) : no_mass();
-            const Mass ml = i < y.L ? kept_mass(at_byte(row, place.l[k]), at_byte(e, place.l[k] / 2)) : no_mass();
-            z.xb[k] = mb.m;
-            z.eb[k] = mb.e;
-            z.xl[k] = ml.m;
-            z.el[k] = ml.e;
+            const int32_t i = i0 + k;
+            // pairs below the first and behind the last have no mass
+            const bool blank = i >= 0 && i <= L, token = i >= 0 && i < L;
+            const int32_t one = token ? y.tokens[i] : 0, before = token && i > 0 ? y.tokens[i - 1] : 0;
+            const int32_t next = i >= -1 && i + 1 < L ? y.tokens[i + 1] : 0;
+            tok[k] = (uint32_t)one < (uint32_t)V ? one : 0;   // (the hypotheses that were scored have no other)
+            skip[k] = token && i > 0 && one != before ? 1.0 : 0.0;
+            skip_up[k] = i >= 0 && i + 1 < L && next != one ? 1.0 : 0.0;
+            live[k] = token ? 1.0 : 0.0;
+            const int32_t bp = blank_place(up, i, L), lp = token_place(up, i, L);
+            fb[k] = blank ? normalized(fm[bp], fe[bp]) : no_mass();
+            bb[k] = blank ? normalized(bm[bp], be[bp]) : no_mass();
+            fl[k] = token ? normalized(fm[lp], fe[lp]) : no_mass();
+            bl[k] = token ? normalized(bm[lp], be[lp]) : no_mass();
         }
     }
-    const Way way = reversed ? ways[1] : ways[0], other = reversed ? ways[0] : ways[1];
-    take_all<K, R, kMeet, TABLE>(z, way, other, y.L, source_of(x, b), wave, used, lds);
+
+    // One exponent for the lane's masses and those that may reach it; whether their spread is within bounds.
+    template <bool UP>
+    __device__ static bool window(const Mass (&b)[K], const Mass (&l)[K], int32_t* E, int32_t* beside) {
+        int32_t top = kNoMass, low = -kNoMass;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            top = max(top, max(b[k].e, l[k].e));
+            low = min(low, min(b[k].e == kNoMass ? -kNoMass : b[k].e, l[k].e == kNoMass ? -kNoMass : l[k].e));
+        }
+        int32_t m = top, n = low;
+#pragma unroll
+        for (int d = 0; d < (R + K - 1) / K; ++d) {
+            m = max(UP ? from_below(m, kNoMass) : from_above(m, kNoMass), top);
+            n = min(UP ? from_below(n, -kNoMass) : from_above(n, -kNoMass), low);
+        }
+        *E = m;
+        *beside = UP ? from_below(m, kNoMass) : from_above(m, kNoMass);
+        return m == kNoMass || m - n <= 1017 - 58 * R;
+    }
+
+    // One frame forwards / the bracket of one frame backwards, with aligned exponents.
+    __device__ void forward(Mass (&b)[K], Mass (&l)[K], const char* row, int32_t type) const {
+        const Mass blank = mass_of(value_at(row, 0, type));
+        const Mass moved = {from_below(l[K - 1].m, 0.0), from_below(l[K - 1].e, kNoMass)};
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k) {
+            const Mass prev = k > 0 ? l[k > 0 ? k - 1 : 0] : moved;
+            Mass stay = plus(l[k], b[k]);
+            if (skip[k] != 0.0) stay = plus(stay, prev);
+            const Mass on = plus(b[k], prev), p = mass_of(value_at(row, tok[k], type));
+            b[k] = normalized(on.m * blank.m, on.e + blank.e);
+            l[k] = live[k] != 0.0 ? normalized(stay.m * p.m, stay.e + p.e) : no_mass();
+        }
+    }
+    __device__ void bracket(Mass (&b)[K], Mass (&l)[K]) const {
+        const Mass up_b = {from_above(b[0].m), from_above(b[0].e, kNoMass)};
+        const Mass up_l = {from_above(l[0].m), from_above(l[0].e, kNoMass)};
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const Mass nb = k + 1 < K ? b[k + 1 < K ? k + 1 : 0] : up_b, nl = k + 1 < K ? l[k + 1 < K ? k + 1 : 0] : up_l;
+            const Mass blank = plus(b[k], l[k]);
+            Mass token = plus(l[k], nb);
+            if (skip_up[k] != 0.0) token = plus(token, nl);
+            b[k] = normalized(blank.m, blank.e);
+            l[k] = live[k] != 0.0 ? normalized(token.m, token.e) : no_mass();
+        }
+    }
+};
+
+constexpr double kOne = 1125899906842624.0;       // 2^50
+constexpr double kShift = 6755399441055744.0;     // 1.5 * 2^52: its last bit is worth one
+
+__device__ inline void add_share(unsigned long long* sum, double share) {
+    const long long a = __double_as_longlong(share + kShift) - __double_as_longlong(kShift);
+    atomicAdd(sum, (unsigned long long)a);
 }
 
-// Occupancies into rows of V sums, which are whole numbers so that the order in which lanes add does not matter.
-// A wavefront takes `per_wave` frames of an utterance at a time: each token's place is read once for all of them.
-constexpr int kGradWaves = 4;   // two where a frame's row takes 32 KB
-constexpr int kGradFrames = 8;
-
-// Orders a wavefront's accesses to its own part of LDS, lane by lane.
-__device__ inline void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-template <typename T>
-__global__ __launch_bounds__(kGradWaves* kWave) void score_grad_kernel(fltop_rows x, fltop_hypotheses h,
-                                                                       const double* grad_scores, ScoreSpace ws,
-                                                                       int32_t per_wave, int32_t chunks, int32_t per_used,
-                                                                       T* grad) {
+template <typename T, int R, bool TABLE>
+__global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, fltop_hypotheses h,
+                                                                  const double* grad_scores, ScoreSpace ws, int32_t blocks,
+                                                                  int32_t parts, T* grad) {
+    constexpr int K = kGradPairs, kWaves = kGradThreads / kWave;
+    constexpr int kPairs = kWave * K, kStep = kPairs - 2 * R;   // of a chunk, and from one to the next
     extern __shared__ char dynamic[];
+    __shared__ double of_wave[kWaves];
+    __shared__ int32_t wide;
+    // the vocabulary is taken in `parts` ranges where a block's sums would not fit
+    const int32_t width = (x.V + parts - 1) / parts;
+    unsigned long long* const sums = reinterpret_cast<unsigned long long*>(dynamic);   // [R][width]
+    double* const table = reinterpret_cast<double*>(sums + R * width);                 // [R][kTabulated]
     const int lane = threadIdx.x & (kWave - 1);
-    const int wave = threadIdx.x / kWave;
-    unsigned long long* sums = reinterpret_cast<unsigned long long*>(dynamic) + (int64_t)wave * per_wave * x.V;
-    const int64_t chunk = (int64_t)blockIdx.x * (blockDim.x / kWave) + wave;
-    const int32_t b = (int32_t)(chunk / chunks), t0 = (int32_t)(chunk % chunks) * per_wave;
-    if (b >= x.B) return;
-    const int32_t frames = min(x.lengths[b], x.T);
-    const int32_t nf = min(per_wave, x.T - t0), live = min(nf, frames - t0);
-    T* out = grad + ((int64_t)b * x.T + t0) * x.V;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t group = blockIdx.x / parts;
+    const int32_t v0 = (int32_t)(blockIdx.x % parts) * width, v1 = min(v0 + width, x.V);
+    const int32_t b = (int32_t)(group / blocks), q = (int32_t)(group % blocks), t0 = q * R;
+    const int32_t frames = __builtin_amdgcn_readfirstlane(min(x.lengths[b], x.T));
+    const int32_t rows = min(R, x.T - t0), nf = min(R, frames - t0);
+    T* const out = grad + ((int64_t)b * x.T + t0) * x.V;
     double most = 0.0;
     bool odd = false;
-    for (int32_t n = lane; n < h.N; n += kWave) {
+    for (int32_t n = threadIdx.x; n < h.N; n += kGradThreads) {
         const int64_t at = (int64_t)b * h.N + n;
         if (ws.total_e[at] <= kNoMass) continue;
         const double w = fabs(grad_scores[at]);
         odd |= !(w <= 1.7976931348623157e308);
         most = fmax(most, w);
     }
-    odd = __any(odd);
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) most = fmax(most, __shfl_xor(most, o, kWave));
-    if (odd || most == 0.0 || live <= 0) {
-        for (int32_t v = lane; v < nf * x.V; v += kWave)
-            out[v] = from_float<T>(odd && v < (int64_t)live * x.V ? NAN : 0.0f);
+    if (lane == 0) of_wave[wave] = most;
+    odd = __syncthreads_or(odd);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most = fmax(most, of_wave[w]);
+    if (odd || most == 0.0 || nf <= 0) {
+        for (int32_t f = 0; f < rows; ++f)
+            for (int32_t v = v0 + threadIdx.x; v < v1; v += kGradThreads)
+                out[(int64_t)f * x.V + v] = from_float<T>(odd && f < nf ? NAN : 0.0f);
         return;
     }
-    for (int32_t v = lane; v < nf * x.V; v += kWave) sums[v] = 0;
-    wave_fence();
-    constexpr double kOne = 1125899906842624.0;       // 2^50
-    constexpr double kShift = 6755399441055744.0;     // 1.5 * 2^52: its last bit is worth one
-    const int64_t row = share_row(h.U);
+    const Source from = source_of(x, b);
+    for (int32_t i = threadIdx.x; i < R * width; i += kGradThreads) sums[i] = 0;
+    if constexpr (TABLE) {
+        bool near = true;
+        for (int32_t f = wave; f < nf; f += kWaves) {
+            const float lp = value_at(from.rows + (int64_t)(t0 + f) * from.frame_bytes, min(lane, x.V - 1), x.type);
+            near &= lp >= kLeastNear && lp <= kMostNear;
+            table[f * kTabulated + lane] = exp_any(lp);
+        }
+        const bool out_of_range = __syncthreads_or(!near);
+        if (threadIdx.x == 0) wide = out_of_range;
+    }
+    __syncthreads();
+    int32_t task = 0;   // chunks of hypotheses, one wavefront after the other
     for (int32_t n = 0; n < h.N; ++n) {
         const int64_t at = (int64_t)b * h.N + n;
-        if (ws.total_e[at] <= kNoMass) continue;
-        // shares come times the mantissa of P, which is at least 1/2
-        const double w = grad_scores[at] / most * (kOne / ws.total_m[at]);
+        const int32_t total_e = __builtin_amdgcn_readfirstlane(ws.total_e[at]);
+        if (total_e <= kNoMass) continue;
         const Hyp y = hypothesis(x, h, b, n);
-        const float* from = ws.shares + (at * x.T + t0) * row;
-        for (int32_t i = lane; i < y.L; i += kWave) {
-            const int32_t v = y.tokens[i];
-            if ((uint32_t)v >= (uint32_t)x.V) continue;   // not the hypotheses that were scored
-            float share[kGradFrames];
+        const double w = grad_scores[at] / most * (kOne / ws.total_m[at]);
+        if (y.L < 0) continue;
+        // one chunk if the pairs fit, else chunks of which R pairs at either end are only passed through
+        const bool one = y.L + 1 <= kPairs;
+        const int32_t chunks = one ? 1 : (y.L + kStep) / kStep;
+        for (int32_t c = 0; c < chunks; ++c, ++task) {
+            if (task % kWaves != wave) continue;
+            const int32_t first = one ? 0 : c * kStep - R;
+            const Chunk<K, R> z(y, ws, at, h.U, x.V, q, first);
+            // whether this lane's pairs are the chunk's own
+            bool own[K];
 #pragma unroll
-            for (int f = 0; f < kGradFrames; ++f) share[f] = f < live ? from[f * row + i] : 0.0f;
-#pragma unroll
-            for (int f = 0; f < kGradFrames; ++f) {
-                if (f >= live) break;
-                const long long a = __double_as_longlong(share[f] * w + kShift) - __double_as_longlong(kShift);
-                atomicAdd(&sums[f * x.V + v], (unsigned long long)a);
+            for (int k = 0; k < K; ++k) {
+                const int32_t i = z.i0 + k;
+                own[k] = one ? i <= y.L : i >= c * kStep && i < (c + 1) * kStep && i <= y.L;
             }
-        }
-        // the blanks: one partial sum from each wavefront that this hypothesis had
-        const int32_t used = y.L / per_used + 1;
-        for (int32_t i = lane; i < live * kShareBlanks; i += kWave) {
-            const int32_t f = i / kShareBlanks, s = i % kShareBlanks;
-            if (s >= used) continue;
-            const long long a =
-                __double_as_longlong(from[f * row + h.U + s] * w + kShift) - __double_as_longlong(kShift);
-            atomicAdd(&sums[f * x.V], (unsigned long long)a);
+            int32_t Ef, Eb, below, above;
+            bool fine = Chunk<K, R>::template window<true>(z.fb, z.fl, &Ef, &below);
+            fine &= Chunk<K, R>::template window<false>(z.bb, z.bl, &Eb, &above);
+            const int32_t shift = share_shift(Ef, Eb, total_e);
+            fine &= shift <= kMostShift && nf == R;
+            // emissions
+            uint32_t raw[TABLE ? 1 : R][K], raw_blank = 0;
+            if constexpr (!TABLE) {
+#pragma unroll
+                for (int f = 0; f < R; ++f) {
+                    const char* row = from.rows + (int64_t)(t0 + min(f, nf - 1)) * from.frame_bytes;
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+                        raw[f][k] = x.type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, z.tok[k])
+                                                             : raw_at<FLTOP_TYPE_F16>(row, z.tok[k]);
+                }
+                const char* row = from.rows + (int64_t)(t0 + min((int32_t)(lane & (R - 1)), nf - 1)) * from.frame_bytes;
+                raw_blank = x.type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, 0) : raw_at<FLTOP_TYPE_F16>(row, 0);
+                float most_lp = raw_value(raw_blank, x.type), least_lp = most_lp;
+#pragma unroll
+                for (int f = 0; f < R; ++f)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        most_lp = fmaxf(most_lp, raw_value(raw[f][k], x.type));
+                        least_lp = fminf(least_lp, raw_value(raw[f][k], x.type));
+                    }
+                fine &= least_lp >= kLeastNear && most_lp <= kMostNear;
+            } else {
+                fine &= !wide;
+            }
+            double blanks[R];
+            if (__all(fine)) {
+                double p[R][K], pb[R];
+                double blank_by_lane = 0.0;
+                if constexpr (!TABLE) blank_by_lane = exp_near(raw_value(raw_blank, x.type));
+#pragma unroll
+                for (int f = 0; f < R; ++f) {
+                    if constexpr (TABLE) {
+                        pb[f] = table[f * kTabulated];
+#pragma unroll
+                        for (int k = 0; k < K; ++k) p[f][k] = table[f * kTabulated + z.tok[k]];
+                    } else {
+                        pb[f] = from_lane(blank_by_lane, f);
+#pragma unroll
+                        for (int k = 0; k < K; ++k) p[f][k] = exp_near(raw_value(raw[f][k], x.type));
+                    }
+                }
+                const double fx = rescaling(below - Ef), fskip = fx * z.skip[0];
+                const double gx = rescaling(above - Eb), gskip = gx * z.skip_up[K - 1];
+                double xb[K], xl[K], ub[K], ul[K], kb[R][K], kl[R][K];
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    xb[k] = ldexp(z.fb[k].m, z.fb[k].e - Ef);
+                    xl[k] = ldexp(z.fl[k].m, z.fl[k].e - Ef);
+                    ub[k] = ldexp(z.bb[k].m, z.bb[k].e - Eb);
+                    ul[k] = ldexp(z.bl[k].m, z.bl[k].e - Eb);
+                }
+#pragma unroll
+                for (int f = 0; f < R; ++f) {
+                    const double moved = from_below(xl[K - 1], 0.0);
+#pragma unroll
+                    for (int k = K - 1; k >= 0; --k) {
+                        const double prev = k > 0 ? xl[k > 0 ? k - 1 : 0] : moved;
+                        const double stay = fma(xb[k], z.live[k], xl[k]);
+                        const double l = fma(prev, k > 0 ? z.skip[k] : fskip, stay);
+                        const double on = k > 0 ? xb[k] + prev : fma(prev, fx, xb[k]);
+                        kb[f][k] = xb[k] = on * pb[f];
+                        kl[f][k] = xl[k] = l * p[f][k];
+                    }
+                }
+                const double factor = shift < -1000 ? 0.0 : power_of_two(min(shift, kMostShift));
+#pragma unroll
+                for (int f = R - 1; f >= 0; --f) {
+                    const double up_b = from_above(ub[0]), up_l = from_above(ul[0]);
+                    blanks[f] = 0.0;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        const double nb = k + 1 < K ? ub[k + 1 < K ? k + 1 : 0] : up_b * gx;
+                        const double nl = k + 1 < K ? ul[k + 1 < K ? k + 1 : 0] : up_l;
+                        const double blank = ub[k] + ul[k];
+                        const double token =
+                            fma(nl, k + 1 < K ? z.skip_up[k] : gskip, fma(nb, z.live[k], ul[k]));
+                        const double sb = kb[f][k] * factor * blank, sl = kl[f][k] * factor * token;
+                        blanks[f] += own[k] ? sb : 0.0;
+                        const int32_t v = z.tok[k] - v0;
+                        if (own[k] && z.live[k] != 0.0 && (uint32_t)v < (uint32_t)(v1 - v0))
+                            add_share(&sums[f * width + v], sl * w);
+                        ub[k] = blank * pb[f];
+                        ul[k] = token * p[f][k];
+                    }
+                }
+            } else {
+                Mass ub[K], ul[K];
+#pragma unroll
+                for (int k = 0; k < K; ++k) ub[k] = z.bb[k], ul[k] = z.bl[k];
+#pragma unroll
+                for (int f = 0; f < R; ++f) blanks[f] = 0.0;
+#pragma unroll 1
+                for (int f = nf - 1; f >= 0; --f) {
+                    Mass kb[K], kl[K];   // forwards once more from the border to this frame
+#pragma unroll
+                    for (int k = 0; k < K; ++k) kb[k] = z.fb[k], kl[k] = z.fl[k];
+#pragma unroll 1
+                    for (int g = 0; g <= f; ++g)
+                        z.forward(kb, kl, from.rows + (int64_t)(t0 + g) * from.frame_bytes, x.type);
+                    z.bracket(ub, ul);
+                    const char* row = from.rows + (int64_t)(t0 + f) * from.frame_bytes;
+                    const Mass pb = mass_of(value_at(row, 0, x.type));
+                    double blank = 0.0;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        if (own[k]) blank += ldexp(kb[k].m * ub[k].m, kb[k].e + ub[k].e - total_e);
+                        const int32_t v = z.tok[k] - v0;
+                        if (own[k] && z.live[k] != 0.0 && (uint32_t)v < (uint32_t)(v1 - v0))
+                            add_share(&sums[f * width + v], ldexp(kl[k].m * ul[k].m, kl[k].e + ul[k].e - total_e) * w);
+                        const Mass p = mass_of(value_at(row, z.tok[k], x.type));
+                        ub[k] = normalized(ub[k].m * pb.m, ub[k].e + pb.e);
+                        ul[k] = normalized(ul[k].m * p.m, ul[k].e + p.e);
+                    }
+#pragma unroll
+                    for (int g = 0; g < R; ++g) blanks[g] = g == f ? blank : blanks[g];
+                }
+            }
+            const double sum = sums_by_lane<R>(blanks);
+            if (v0 == 0 && lane < nf) add_share(&sums[lane * width], sum * w);
         }
     }
-    wave_fence();
-    for (int32_t v = lane; v < nf * x.V; v += kWave)
-        out[v] = from_float<T>((float)((double)(long long)sums[v] * (most / kOne)));
+    __syncthreads();
+    for (int32_t f = 0; f < rows; ++f)
+        for (int32_t v = v0 + threadIdx.x; v < v1; v += kGradThreads)
+            out[(int64_t)f * x.V + v] =
+                from_float<T>(f < nf ? (float)((double)(long long)sums[f * width + v - v0] * (most / kOne)) : 0.0f);
 }
 
 // Pairs of a lane, frames of a block, most threads.
 template <int K, int R, int THREADS, bool TABLE>
 struct Build {
+    static unsigned threads(int W) { return 2 * kWave * (TABLE ? W + 1 : W); }
     static hipError_t score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
                             hipStream_t stream) {
         const int W = waves_for(h.U, K);
-        const dim3 grid((unsigned)(x.B * h.N)), block(2 * kWave * W);
-        const size_t bytes = Lds<R>::bytes(W, x.V, h.U, true);
+        const dim3 grid((unsigned)(x.B * h.N)), block(threads(W));
+        const size_t bytes = Lds<R, TABLE>::bytes(W, h.U, true);
         if (keep)
-            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, kKeep>), grid, block, bytes, stream, x, h, out_scores,
+            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, true>), grid, block, bytes, stream, x, h, out_scores,
                                *keep);
         else
-            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, kScore>), grid, block, bytes, stream, x, h, out_scores,
+            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, false>), grid, block, bytes, stream, x, h, out_scores,
                                ScoreSpace{});
-        return hipGetLastError();
-    }
-    static hipError_t shares(const fltop_rows& x, const fltop_hypotheses& h, const ScoreSpace& ws, hipStream_t stream) {
-        const int W = waves_for(h.U, K);
-        hipLaunchKernelGGL((shares_kernel<K, R, THREADS, TABLE>), dim3((unsigned)(x.B * h.N)), dim3(2 * kWave * W),
-                           Lds<R>::bytes(W, x.V, h.U, false), stream, x, h, ws);
         return hipGetLastError();
     }
 };
@@ -966,28 +1137,35 @@ template <typename F>
 hipError_t with_build(const fltop_rows& x, const fltop_hypotheses& h, F f) {
     const bool table = x.V <= kTabulated;
     switch (lattice_pairs(x.B, h.N, h.U)) {
-        case 1: return table ? f(Build<1, 8, 256, true>{}) : f(Build<1, 8, 256, false>{});
-        case 2: return table ? f(Build<2, 8, 256, true>{}) : f(Build<2, 8, 256, false>{});
-        case 4: return table ? f(Build<4, 4, 256, true>{}) : f(Build<4, 4, 256, false>{});
+        case 2: return table ? f(Build<2, 8, 384, true>{}) : f(Build<2, 8, 256, false>{});
+        case 4: return table ? f(Build<4, 4, 384, true>{}) : f(Build<4, 4, 256, false>{});
         default:
-            if (waves_for(h.U, 8) <= 2) return table ? f(Build<8, 4, 256, true>{}) : f(Build<8, 4, 256, false>{});
-            return table ? f(Build<8, 4, 1024, true>{}) : f(Build<8, 4, 1024, false>{});
+            if (waves_for(h.U, 8) <= 2) return table ? f(Build<8, 4, 384, true>{}) : f(Build<8, 4, 256, false>{});
+            return f(Build<8, 4, 1024, false>{});
     }
+}
+
+template <typename T, int R, bool TABLE>
+hipError_t grad_as(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores, const ScoreSpace& ws,
+                   void* grad, hipStream_t stream) {
+    // ranges of the vocabulary whose sums take at most 64 KB
+    const int32_t parts = (x.V * R * 8 + 65535) / 65536, width = (x.V + parts - 1) / parts;
+    const int32_t blocks = (int32_t)blocks_of(x.T, R);
+    const size_t bytes = (size_t)R * width * 8 + (TABLE ? R * kTabulated * 8 : 0);
+    hipLaunchKernelGGL((score_grad_kernel<T, R, TABLE>), dim3((unsigned)(x.B * (int64_t)blocks * parts)),
+                       dim3(kGradThreads), bytes, stream, x, h, grad_scores, ws, blocks, parts, static_cast<T*>(grad));
+    return hipGetLastError();
 }
 
 template <typename T>
 hipError_t grad_of(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores, const ScoreSpace& ws,
                    void* grad, hipStream_t stream) {
-    // frames of a wavefront: as many as fit 16 KB (a workgroup's 64 KB leave room for two on a compute unit)
-    int32_t per_wave = 2048 / x.V;
-    per_wave = per_wave < 1 ? 1 : per_wave > kGradFrames ? kGradFrames : per_wave;
-    const int32_t chunks = (x.T + per_wave - 1) / per_wave;
-    const int waves = x.V > 2048 ? 2 : kGradWaves;
-    const int64_t blocks = ((int64_t)x.B * chunks + waves - 1) / waves;
-    hipLaunchKernelGGL(score_grad_kernel<T>, dim3((unsigned)blocks), dim3(waves * kWave),
-                       (size_t)waves * per_wave * x.V * sizeof(unsigned long long), stream, x, h, grad_scores, ws,
-                       per_wave, chunks, kWave * lattice_pairs(x.B, h.N, h.U), static_cast<T*>(grad));
-    return hipGetLastError();
+    const bool table = x.V <= kTabulated;
+    if (block_frames(lattice_pairs(x.B, h.N, h.U)) == 8)
+        return table ? grad_as<T, 8, true>(x, h, grad_scores, ws, grad, stream)
+                     : grad_as<T, 8, false>(x, h, grad_scores, ws, grad, stream);
+    return table ? grad_as<T, 4, true>(x, h, grad_scores, ws, grad, stream)
+                 : grad_as<T, 4, false>(x, h, grad_scores, ws, grad, stream);
 }
 
 }  // namespace
@@ -999,8 +1177,6 @@ hipError_t launch_score(const fltop_rows& x, const fltop_hypotheses& h, double* 
 
 hipError_t launch_score_grad(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores,
                              const ScoreSpace& ws, void* grad, hipStream_t stream) {
-    const hipError_t e = with_build(x, h, [&](auto build) { return decltype(build)::shares(x, h, ws, stream); });
-    if (e != hipSuccess) return e;
     if (x.type == FLTOP_TYPE_BF16) return grad_of<__hip_bfloat16>(x, h, grad_scores, ws, grad, stream);
     if (x.type == FLTOP_TYPE_F16) return grad_of<__half>(x, h, grad_scores, ws, grad, stream);
     return grad_of<float>(x, h, grad_scores, ws, grad, stream);

@@ -41,7 +41,7 @@ BAD_ROWS = [({"data": None}, NULL), ({"lengths": None}, NULL), ({"B": 0}, SHAPE)
             ({"V": binding.MAX_VOCAB + 1}, VOCAB), ({"type": 3}, OPTION), ({"type": -1}, OPTION)]
 BAD_HYPS = [({"tokens": None}, NULL), ({"lengths": None}, NULL), ({"N": 0}, SHAPE), ({"U": 0}, SHAPE),
             ({"U": binding.MAX_LABELS + 1}, SHAPE), ({"token_stride": -8}, SHAPE), ({"token_batch_stride": -1}, SHAPE),
-            ({"length_batch_stride": -1}, SHAPE), ({"N": 1 << 30}, SHAPE)]
+            ({"length_batch_stride": -1}, SHAPE), ({"N": binding.MAX_BEAM + 1}, BEAM)]
 
 
 def test_score_refusals(lib):
@@ -70,7 +70,7 @@ def test_score_refusals(lib):
 def test_workspace_sizes(lib):
     assert lib.fltop_ctc_score_workspace_bytes(2, 10, 3, 8) % 256 == 0
     for bad in ((0, 10, 3, 8), (2, 0, 3, 8), (2, 10, 0, 8), (2, 10, 3, 0), (2, 10, 3, binding.MAX_LABELS + 1),
-                (1 << 20, 10, 1 << 20, 8)):
+                (1 << 30, 10, 1024, 8), (2, 10, binding.MAX_BEAM + 1, 8)):
         assert lib.fltop_ctc_score_workspace_bytes(*bad) == 0
     # beyond 32 bits
     assert lib.fltop_ctc_score_workspace_bytes(256, 1500, 8, 700) > 256 * 1500 * 8 * 1401 * 8
