@@ -76,23 +76,25 @@ __device__ inline Mass plus(Mass a, Mass b) {
 
 constexpr int kMostWaves = 8;   // wavefronts that one direction of a lattice takes
 
+// Masses of a pair of states (a blank and the token behind it) at the border of a block of frames: b 2^eb, l 2^el.
+struct alignas(8) Mark {
+    double b, l;
+    int32_t eb, el;
+};
+
 // What fltop_ctc_score leaves for fltop_ctc_score_grad.
 struct ScoreSpace {
     double* total_m;   // [B*N] P(hypothesis) as a Mass; kNoMass for one that takes no part
     int32_t* total_e;  // [B*N]
-    double* marks;     // [B*N][2][blocks][row] masses of both directions at the borders of blocks of frames
-    int32_t* mark_exps;   // their exponents, alike
-    int64_t row;       // 2U + 1 states and a place for what has no meaning
-    int64_t marks_of;  // places of one direction of one hypothesis
+    Mark* marks;       // [B*N][2][blocks][row] both directions at the borders of blocks
+    int64_t row;       // pairs that a direction's lanes hold
+    int64_t marks_of;  // marks of one direction of one hypothesis
     size_t bytes;
 };
 
-// Pairs of states that a lane holds: as few as keep a direction within two wavefronts, so that each of a
-// workgroup's wavefronts has a SIMD for itself (eight of eight pairs beyond 1023 tokens).
-inline int lattice_pairs(int32_t B, int32_t N, int32_t U) {
-    (void)B, (void)N;
-    return U < 256 ? 2 : U < 512 ? 4 : 8;
-}
+// Pairs of states that a lane holds: as few as keep a direction within four wavefronts (eight of eight pairs beyond
+// 1023 tokens).
+inline int lattice_pairs(int32_t U) { return U < 512 ? 2 : U < 1024 ? 4 : 8; }
 inline int waves_for(int32_t U, int pairs) { return (U + 64 * pairs) / (64 * pairs); }   // for U + 1 pairs
 // Frames that are gone through together: exponents are kept once for each such block.
 inline int block_frames(int pairs) { return pairs < 4 ? 8 : 4; }
@@ -101,18 +103,16 @@ __host__ __device__ inline int64_t blocks_of(int32_t T, int32_t R) { return ((in
 inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32_t U) {
     ScoreSpace s;
     const size_t hyps = (size_t)B * (size_t)N;
-    s.row = 2 * (int64_t)U + 2;
-    s.marks_of = blocks_of(T, block_frames(lattice_pairs(B, N, U))) * s.row;
+    const int pairs = lattice_pairs(U);
+    s.row = (int64_t)pairs * waves_for(U, pairs) * 64;
+    s.marks_of = blocks_of(T, block_frames(pairs)) * s.row;
     const size_t off_e = align_up(hyps * sizeof(double), 256);
     const size_t off_marks = off_e + align_up(hyps * sizeof(int32_t), 256);
-    const size_t places = hyps * 2 * (size_t)s.marks_of;
-    const size_t off_exps = off_marks + align_up(places * sizeof(double), 256);
-    s.bytes = off_exps + align_up(places * sizeof(int32_t), 256);
+    s.bytes = align_up(off_marks + hyps * 2 * (size_t)s.marks_of * sizeof(Mark), 256);
     char* p = static_cast<char*>(base);
     s.total_m = p ? reinterpret_cast<double*>(p) : nullptr;
     s.total_e = p ? reinterpret_cast<int32_t*>(p + off_e) : nullptr;
-    s.marks = p ? reinterpret_cast<double*>(p + off_marks) : nullptr;
-    s.mark_exps = p ? reinterpret_cast<int32_t*>(p + off_exps) : nullptr;
+    s.marks = p ? reinterpret_cast<Mark*>(p + off_marks) : nullptr;
     return s;
 }
 

@@ -119,11 +119,9 @@ __device__ inline double exp_near(float lp) {
     return from_words((int32_t)(bits >> 32) + ((int32_t)__double_as_longlong(t) << 20), (int32_t)bits);
 }
 
-// exp(lp) of any emission: 0 or infinity where it leaves the range in which blocks are gone through with one exponent.
-__device__ inline double exp_any(float lp) {
-    const double near = exp_near(fminf(fmaxf(lp, -600.0f), 600.0f));
-    return lp < -600.0f ? 0.0 : lp <= 600.0f ? near : INFINITY;
-}
+// exp(lp) of any emission, off where it leaves the range in which blocks are gone through with one exponent (and still
+// outside of that range).
+__device__ inline double exp_any(float lp) { return exp_near(fminf(fmaxf(lp, -600.0f), 600.0f)); }
 
 // An element as it lies in memory; converted where it is used, so that loads stay in flight.
 template <int TYPE>
@@ -132,6 +130,12 @@ __device__ inline uint32_t raw_at(const char* row, int32_t v) {
         return reinterpret_cast<const uint32_t*>(row)[v];
     else
         return reinterpret_cast<const uint16_t*>(row)[v];
+}
+template <int TYPE>
+__device__ inline float raw_as(uint32_t x) {
+    if constexpr (TYPE == FLTOP_TYPE_F32) return __uint_as_float(x);
+    if constexpr (TYPE == FLTOP_TYPE_BF16) return __uint_as_float(x << 16);
+    return __half2float(__ushort_as_half((unsigned short)x));
 }
 __device__ inline float raw_value(uint32_t x, int32_t type) {
     const float half = __half2float(__ushort_as_half((unsigned short)x));
@@ -150,6 +154,17 @@ struct Source {
     const char* rows;
     int64_t frame_bytes;
     int32_t type, V;
+};
+
+// Rows of a block in the order in which a direction takes them; behind its nf frames the last one again.
+struct Rows {
+    const char* row;
+    int64_t step;
+    int32_t left;
+    __device__ Rows(const Source& from, int32_t t0, int32_t nf, bool reversed)
+        : row(from.rows + (int64_t)(reversed ? t0 + nf - 1 : t0) * from.frame_bytes),
+          step(reversed ? -from.frame_bytes : from.frame_bytes), left(nf - 1) {}
+    __device__ void next() { row += left-- > 0 ? step : 0; }
 };
 
 // What the wavefront above needs of a block: the last lane's token mass before each frame.  (Below the first
@@ -198,20 +213,9 @@ struct Lds {
 struct Way {
     int32_t lo, hi;      // its frames
     bool reversed;
-    double* marks;       // masses at the borders of blocks, [blocks][row] (or NULL)
-    int32_t* mark_exps;  // their exponents, alike
+    Mark* marks;         // masses at the borders of blocks, [blocks][row] (or NULL), pair by pair as the direction sees them
     int32_t row;
-    int32_t U;
 };
-
-// Where pair i's states are in a row of border masses: blanks, then tokens, then a place of no meaning for lanes behind
-// the last pair, so that a store needs no branch.
-__device__ inline int32_t blank_place(const Way& way, int32_t i, int32_t L) {
-    return i > L ? way.row - 1 : way.reversed ? L - i : i;
-}
-__device__ inline int32_t token_place(const Way& way, int32_t i, int32_t L) {
-    return i >= L ? way.row - 1 : way.U + 1 + (way.reversed ? L - 1 - i : i);
-}
 
 // The part of the lattice that one lane holds.
 template <int K, int R, bool TABLE>
@@ -260,13 +264,11 @@ struct Lane {
     // Asks for the emissions of frames t0 .. t0 + nf - 1, in the order in which they are taken.
     template <int TYPE>
     __device__ void ask_as(const Source& from, int32_t t0, int32_t nf, bool reversed) {
+        Rows rows(from, t0, nf, reversed);
 #pragma unroll
-        for (int f = 0; f < R; ++f) {
-            const int32_t g = min(f, nf - 1);
-            const char* row = from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes;
+        for (int f = 0; f < R; ++f, rows.next())
 #pragma unroll
-            for (int k = 0; k < K; ++k) raw[TABLE ? 0 : f][k] = raw_at<TYPE>(row, tok[k]);
-        }
+            for (int k = 0; k < K; ++k) raw[TABLE ? 0 : f][k] = raw_at<TYPE>(rows.row, tok[k]);
         const int32_t g = min((int32_t)(threadIdx.x & (R - 1)), nf - 1);
         raw_blank = raw_at<TYPE>(from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes, 0);
     }
@@ -276,12 +278,21 @@ struct Lane {
         else
             ask_as<FLTOP_TYPE_F16>(from, t0, nf, reversed);   // 16 bits of either kind
     }
-    __device__ void got(int32_t type) {
+    template <int TYPE>
+    __device__ void got_as() {
 #pragma unroll
         for (int f = 0; f < R; ++f)
 #pragma unroll
-            for (int k = 0; k < K; ++k) given[f][k] = raw_value(raw[TABLE ? 0 : f][k], type);
-        given_blank[0] = raw_value(raw_blank, type);
+            for (int k = 0; k < K; ++k) given[f][k] = raw_as<TYPE>(raw[TABLE ? 0 : f][k]);
+        given_blank[0] = raw_as<TYPE>(raw_blank);
+    }
+    __device__ void got(int32_t type) {
+        if (type == FLTOP_TYPE_F32)
+            got_as<FLTOP_TYPE_F32>();
+        else if (type == FLTOP_TYPE_BF16)
+            got_as<FLTOP_TYPE_BF16>();
+        else
+            got_as<FLTOP_TYPE_F16>();
     }
     __device__ void look_up(const double* table) {
 #pragma unroll
@@ -408,16 +419,11 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
     const int32_t t0 = q * R;
     const int32_t nf = min(R, way.hi - t0);
     if (way.marks) {
-        double* const m = way.marks + (int64_t)q * way.row;
-        int32_t* const e = way.mark_exps + (int64_t)q * way.row;
+        // (every lane has its place, with or without mass)
+        Mark* const to = way.marks + (int64_t)q * way.row + z.i0;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int32_t bp = blank_place(way, z.i0 + k, L), lp = token_place(way, z.i0 + k, L);
-            m[bp] = z.xb[k];
-            e[bp] = z.common ? z.E : z.eb[k];
-            m[lp] = z.xl[k];
-            e[lp] = z.common ? z.E : z.el[k];
-        }
+        for (int k = 0; k < K; ++k)
+            to[k] = {z.xb[k], z.xl[k], z.common ? z.E : z.eb[k], z.common ? z.E : z.el[k]};
     }
     int32_t E, least, below;
     bool fine = z.enter(in, &E, &least, &below) && nf == R && !in.aligned;
@@ -525,12 +531,9 @@ struct Tabulator {
     template <int TYPE>
     __device__ void ask_as(const Source& from, const Way& way, int32_t q) {
         const int32_t v = min((int32_t)(threadIdx.x & (kWave - 1)), from.V - 1);
-        const int32_t nf = min(R, way.hi - q * R);
+        Rows rows(from, q * R, min(R, way.hi - q * R), way.reversed);
 #pragma unroll
-        for (int f = 0; f < R; ++f) {
-            const int32_t g = min(f, nf - 1);
-            raw[f] = raw_at<TYPE>(from.rows + (int64_t)(q * R + (way.reversed ? nf - 1 - g : g)) * from.frame_bytes, v);
-        }
+        for (int f = 0; f < R; ++f, rows.next()) raw[f] = raw_at<TYPE>(rows.row, v);
     }
     __device__ void ask(const Source& from, const Way& way, int32_t q) {
         if (from.type == FLTOP_TYPE_F32)
@@ -538,17 +541,27 @@ struct Tabulator {
         else
             ask_as<FLTOP_TYPE_F16>(from, way, q);
     }
-    __device__ void put(const Source& from, double* table, int32_t* wide) {
+    template <int TYPE>
+    __device__ void put_as(double* table, int32_t* wide) {
         const int lane = threadIdx.x & (kWave - 1);
-        bool near = true;
+        float most = raw_as<TYPE>(raw[0]), least = most;
 #pragma unroll
         for (int f = 0; f < R; ++f) {
-            const float lp = raw_value(raw[f], from.type);
-            near &= lp >= kLeastNear && lp <= kMostNear;
+            const float lp = raw_as<TYPE>(raw[f]);
+            most = fmaxf(most, lp);
+            least = fminf(least, lp);
             table[f * kTabulated + lane] = exp_any(lp);
         }
-        const bool all = __all(near);
+        const bool all = __all(least >= kLeastNear && most <= kMostNear);
         if (lane == 0) *wide = !all;
+    }
+    __device__ void put(const Source& from, double* table, int32_t* wide) {
+        if (from.type == FLTOP_TYPE_F32)
+            put_as<FLTOP_TYPE_F32>(table, wide);
+        else if (from.type == FLTOP_TYPE_BF16)
+            put_as<FLTOP_TYPE_BF16>(table, wide);
+        else
+            put_as<FLTOP_TYPE_F16>(table, wide);
     }
 };
 
@@ -681,14 +694,9 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
     }
     const int32_t used = y.L / (kWave * K) + 1;
     const int32_t middle = KEEP ? y.frames : middle_of<R>(y.frames);
-    Way forward = {0, middle, false, nullptr, nullptr, (int32_t)ws.row, h.U};
-    Way backward = {KEEP ? 0 : middle, y.frames, true, nullptr, nullptr, (int32_t)ws.row, h.U};
-    if constexpr (KEEP) {
-        forward.marks = ws.marks + at * 2 * ws.marks_of;
-        forward.mark_exps = ws.mark_exps + at * 2 * ws.marks_of;
-        backward.marks = forward.marks + ws.marks_of;
-        backward.mark_exps = forward.mark_exps + ws.marks_of;
-    }
+    Mark* const marks = KEEP ? ws.marks + at * 2 * ws.marks_of : nullptr;
+    const Way forward = {0, middle, false, marks, (int32_t)ws.row};
+    const Way backward = {KEEP ? 0 : middle, y.frames, true, KEEP ? marks + ws.marks_of : nullptr, (int32_t)ws.row};
     const Way way = reversed ? backward : forward, other = reversed ? forward : backward;
     if (role.tabulates) {
         if constexpr (TABLE) tabulate_all<R>(way, other, source_of(x, b), used, lds);
@@ -792,7 +800,7 @@ __global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypo
 // whole numbers: in any order the same.  The conditions for one exponent for each lane are those of the scores'
 // blocks, for both directions, and that P's exponent is within reach of theirs.
 
-constexpr int kGradPairs = 2, kGradThreads = 256;
+constexpr int kGradPairs = 2, kGradThreads = 256;   // (fewer threads where there are fewer chunks)
 
 __device__ inline int32_t from_above(int32_t x, int32_t last) {
     return __builtin_amdgcn_update_dpp(last, x, 0x130, 0xf, 0xf, false);  // wave_shl:1
@@ -819,13 +827,10 @@ struct Chunk {
     double skip[K], skip_up[K], live[K];   // skip_up: of the pair above
     Mass fb[K], fl[K], bb[K], bl[K];       // masses at the lower border (forwards) and the upper one (backwards)
 
-    __device__ Chunk(const Hyp& y, const ScoreSpace& ws, int64_t at, int32_t U, int32_t V, int32_t q, int32_t first_pair)
+    __device__ Chunk(const Hyp& y, const ScoreSpace& ws, int64_t at, int32_t V, int32_t q, int32_t first_pair)
         : i0(first_pair + (int32_t)(threadIdx.x & (kWave - 1)) * K), L(y.L) {
-        const Way up = {0, 0, false, nullptr, nullptr, (int32_t)ws.row, U};
-        const double* fm = ws.marks + at * 2 * ws.marks_of + q * ws.row;
-        const int32_t* fe = ws.mark_exps + at * 2 * ws.marks_of + q * ws.row;
-        const double* bm = fm + ws.marks_of;
-        const int32_t* be = fe + ws.marks_of;
+        const Mark* const fore = ws.marks + at * 2 * ws.marks_of + q * ws.row;
+        const Mark* const back = fore + ws.marks_of;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int32_t i = i0 + k;
@@ -837,11 +842,12 @@ struct Chunk {
             skip[k] = token && i > 0 && one != before ? 1.0 : 0.0;
             skip_up[k] = i >= 0 && i + 1 < L && next != one ? 1.0 : 0.0;
             live[k] = token ? 1.0 : 0.0;
-            const int32_t bp = blank_place(up, i, L), lp = token_place(up, i, L);
-            fb[k] = blank ? normalized(fm[bp], fe[bp]) : no_mass();
-            bb[k] = blank ? normalized(bm[bp], be[bp]) : no_mass();
-            fl[k] = token ? normalized(fm[lp], fe[lp]) : no_mass();
-            bl[k] = token ? normalized(bm[lp], be[lp]) : no_mass();
+            // backwards, pair j is blank L - j and token L - 1 - j
+            const Mark f = fore[min(max(i, 0), L)], u = back[min(max(L - i, 0), L)], v = back[min(max(L - 1 - i, 0), L)];
+            fb[k] = blank ? normalized(f.b, f.eb) : no_mass();
+            fl[k] = token ? normalized(f.l, f.el) : no_mass();
+            bb[k] = blank ? normalized(u.b, u.eb) : no_mass();
+            bl[k] = token ? normalized(v.l, v.el) : no_mass();
         }
     }
 
@@ -903,13 +909,14 @@ __device__ inline void add_share(unsigned long long* sum, double share) {
 }
 
 template <typename T, int R, bool TABLE>
-__global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, fltop_hypotheses h,
+__global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel(fltop_rows x, fltop_hypotheses h,
                                                                   const double* grad_scores, ScoreSpace ws, int32_t blocks,
                                                                   int32_t parts, T* grad) {
-    constexpr int K = kGradPairs, kWaves = kGradThreads / kWave;
+    constexpr int K = kGradPairs;
+    const int kWaves = (int)blockDim.x / kWave;
     constexpr int kPairs = kWave * K, kStep = kPairs - 2 * R;   // of a chunk, and from one to the next
     extern __shared__ char dynamic[];
-    __shared__ double of_wave[kWaves];
+    __shared__ double of_wave[kGradThreads / kWave];
     __shared__ int32_t wide;
     // the vocabulary is taken in `parts` ranges where a block's sums would not fit
     const int32_t width = (x.V + parts - 1) / parts;
@@ -925,7 +932,7 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
     T* const out = grad + ((int64_t)b * x.T + t0) * x.V;
     double most = 0.0;
     bool odd = false;
-    for (int32_t n = threadIdx.x; n < h.N; n += kGradThreads) {
+    for (int32_t n = threadIdx.x; n < h.N; n += blockDim.x) {
         const int64_t at = (int64_t)b * h.N + n;
         if (ws.total_e[at] <= kNoMass) continue;
         const double w = fabs(grad_scores[at]);
@@ -936,16 +943,15 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
     for (int o = kWave / 2; o > 0; o >>= 1) most = fmax(most, __shfl_xor(most, o, kWave));
     if (lane == 0) of_wave[wave] = most;
     odd = __syncthreads_or(odd);
-#pragma unroll
     for (int w = 0; w < kWaves; ++w) most = fmax(most, of_wave[w]);
     if (odd || most == 0.0 || nf <= 0) {
         for (int32_t f = 0; f < rows; ++f)
-            for (int32_t v = v0 + threadIdx.x; v < v1; v += kGradThreads)
+            for (int32_t v = v0 + threadIdx.x; v < v1; v += blockDim.x)
                 out[(int64_t)f * x.V + v] = from_float<T>(odd && f < nf ? NAN : 0.0f);
         return;
     }
     const Source from = source_of(x, b);
-    for (int32_t i = threadIdx.x; i < R * width; i += kGradThreads) sums[i] = 0;
+    for (int32_t i = threadIdx.x; i < R * width; i += blockDim.x) sums[i] = 0;
     if constexpr (TABLE) {
         bool near = true;
         for (int32_t f = wave; f < nf; f += kWaves) {
@@ -971,7 +977,7 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
         for (int32_t c = 0; c < chunks; ++c, ++task) {
             if (task % kWaves != wave) continue;
             const int32_t first = one ? 0 : c * kStep - R;
-            const Chunk<K, R> z(y, ws, at, h.U, x.V, q, first);
+            const Chunk<K, R> z(y, ws, at, x.V, q, first);
             // whether this lane's pairs are the chunk's own
             bool own[K];
 #pragma unroll
@@ -1011,21 +1017,19 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
             }
             double blanks[R];
             if (__all(fine)) {
-                double p[R][K], pb[R];
+                double p[TABLE ? 1 : R][K], pb[TABLE ? 1 : R];   // (a table is read again)
                 double blank_by_lane = 0.0;
                 if constexpr (!TABLE) blank_by_lane = exp_near(raw_value(raw_blank, x.type));
+                if constexpr (!TABLE) {
 #pragma unroll
-                for (int f = 0; f < R; ++f) {
-                    if constexpr (TABLE) {
-                        pb[f] = table[f * kTabulated];
-#pragma unroll
-                        for (int k = 0; k < K; ++k) p[f][k] = table[f * kTabulated + z.tok[k]];
-                    } else {
+                    for (int f = 0; f < R; ++f) {
                         pb[f] = from_lane(blank_by_lane, f);
 #pragma unroll
                         for (int k = 0; k < K; ++k) p[f][k] = exp_near(raw_value(raw[f][k], x.type));
                     }
                 }
+                auto blank_p = [&](int f) { return TABLE ? table[f * kTabulated] : pb[TABLE ? 0 : f]; };
+                auto token_p = [&](int f, int k) { return TABLE ? table[f * kTabulated + z.tok[k]] : p[TABLE ? 0 : f][k]; };
                 const double fx = rescaling(below - Ef), fskip = fx * z.skip[0];
                 const double gx = rescaling(above - Eb), gskip = gx * z.skip_up[K - 1];
                 double xb[K], xl[K], ub[K], ul[K], kb[R][K], kl[R][K];
@@ -1045,8 +1049,8 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
                         const double stay = fma(xb[k], z.live[k], xl[k]);
                         const double l = fma(prev, k > 0 ? z.skip[k] : fskip, stay);
                         const double on = k > 0 ? xb[k] + prev : fma(prev, fx, xb[k]);
-                        kb[f][k] = xb[k] = on * pb[f];
-                        kl[f][k] = xl[k] = l * p[f][k];
+                        kb[f][k] = xb[k] = on * blank_p(f);
+                        kl[f][k] = xl[k] = l * token_p(f, k);
                     }
                 }
                 const double factor = shift < -1000 ? 0.0 : power_of_two(min(shift, kMostShift));
@@ -1066,8 +1070,8 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
                         const int32_t v = z.tok[k] - v0;
                         if (own[k] && z.live[k] != 0.0 && (uint32_t)v < (uint32_t)(v1 - v0))
                             add_share(&sums[f * width + v], sl * w);
-                        ub[k] = blank * pb[f];
-                        ul[k] = token * p[f][k];
+                        ub[k] = blank * blank_p(f);
+                        ul[k] = token * token_p(f, k);
                     }
                 }
             } else {
@@ -1108,7 +1112,7 @@ __global__ __launch_bounds__(kGradThreads) void score_grad_kernel(fltop_rows x, 
     }
     __syncthreads();
     for (int32_t f = 0; f < rows; ++f)
-        for (int32_t v = v0 + threadIdx.x; v < v1; v += kGradThreads)
+        for (int32_t v = v0 + threadIdx.x; v < v1; v += blockDim.x)
             out[(int64_t)f * x.V + v] =
                 from_float<T>(f < nf ? (float)((double)(long long)sums[f * width + v - v0] * (most / kOne)) : 0.0f);
 }
@@ -1136,12 +1140,10 @@ struct Build {
 template <typename F>
 hipError_t with_build(const fltop_rows& x, const fltop_hypotheses& h, F f) {
     const bool table = x.V <= kTabulated;
-    switch (lattice_pairs(x.B, h.N, h.U)) {
-        case 2: return table ? f(Build<2, 8, 384, true>{}) : f(Build<2, 8, 256, false>{});
-        case 4: return table ? f(Build<4, 4, 384, true>{}) : f(Build<4, 4, 256, false>{});
-        default:
-            if (waves_for(h.U, 8) <= 2) return table ? f(Build<8, 4, 384, true>{}) : f(Build<8, 4, 256, false>{});
-            return f(Build<8, 4, 1024, false>{});
+    switch (lattice_pairs(h.U)) {
+        case 2: return table ? f(Build<2, 8, 640, true>{}) : f(Build<2, 8, 512, false>{});
+        case 4: return table ? f(Build<4, 4, 640, true>{}) : f(Build<4, 4, 512, false>{});
+        default: return f(Build<8, 4, 1024, false>{});
     }
 }
 
@@ -1152,8 +1154,10 @@ hipError_t grad_as(const fltop_rows& x, const fltop_hypotheses& h, const double*
     const int32_t parts = (x.V * R * 8 + 65535) / 65536, width = (x.V + parts - 1) / parts;
     const int32_t blocks = (int32_t)blocks_of(x.T, R);
     const size_t bytes = (size_t)R * width * 8 + (TABLE ? R * kTabulated * 8 : 0);
-    hipLaunchKernelGGL((score_grad_kernel<T, R, TABLE>), dim3((unsigned)(x.B * (int64_t)blocks * parts)),
-                       dim3(kGradThreads), bytes, stream, x, h, grad_scores, ws, blocks, parts, static_cast<T*>(grad));
+    // as many wavefronts as there may be chunks
+    const int64_t chunks = (int64_t)h.N * ((h.U + 1) / (kWave * kGradPairs - 2 * R) + 1);
+    const unsigned threads = chunks < kGradThreads / kWave ? (unsigned)chunks * kWave : kGradThreads;
+    hipLaunchKernelGGL((score_grad_kernel<T, R, TABLE>), dim3((unsigned)(x.B * (int64_t)blocks * parts)), dim3(threads), bytes, stream, x, h, grad_scores, ws, blocks, parts, static_cast<T*>(grad));
     return hipGetLastError();
 }
 
@@ -1161,7 +1165,7 @@ template <typename T>
 hipError_t grad_of(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores, const ScoreSpace& ws,
                    void* grad, hipStream_t stream) {
     const bool table = x.V <= kTabulated;
-    if (block_frames(lattice_pairs(x.B, h.N, h.U)) == 8)
+    if (block_frames(lattice_pairs(h.U)) == 8)
         return table ? grad_as<T, 8, true>(x, h, grad_scores, ws, grad, stream)
                      : grad_as<T, 8, false>(x, h, grad_scores, ws, grad, stream);
     return table ? grad_as<T, 4, true>(x, h, grad_scores, ws, grad, stream)
