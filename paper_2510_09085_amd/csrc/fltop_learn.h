@@ -92,9 +92,8 @@ struct ScoreSpace {
     size_t bytes;
 };
 
-// Pairs of states that a lane holds: as few as keep a direction within four wavefronts (eight of eight pairs beyond
-// 1023 tokens).
-inline int lattice_pairs(int32_t U) { return U < 512 ? 2 : U < 1024 ? 4 : 8; }
+// Pairs of states that a lane holds: two while a direction, and a wavefront that tabulates for it, have eight at most.
+inline int lattice_pairs(int32_t U) { return U < 896 ? 2 : U < 1024 ? 4 : 8; }
 inline int waves_for(int32_t U, int pairs) { return (U + 64 * pairs) / (64 * pairs); }   // for U + 1 pairs
 // Frames that are gone through together: exponents are kept once for each such block.
 inline int block_frames(int pairs) { return pairs < 4 ? 8 : 4; }

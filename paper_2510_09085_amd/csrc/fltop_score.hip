@@ -1141,7 +1141,13 @@ template <typename F>
 hipError_t with_build(const fltop_rows& x, const fltop_hypotheses& h, F f) {
     const bool table = x.V <= kTabulated;
     switch (lattice_pairs(h.U)) {
-        case 2: return table ? f(Build<2, 8, 640, true>{}) : f(Build<2, 8, 512, false>{});
+        case 2:
+            // Registers for three wavefronts a SIMD, without spills, where a direction has four at most and the hypotheses do
+            // not fill the chip twice (64 transcripts of 229 tokens: 104 us, 128 with the other build); else for four, of up to
+            // seven a direction (2048 hypotheses of 229: 300 us, 384 with the first).
+            if (h.U < 512 && (int64_t)x.B * h.N < 512)
+                return table ? f(Build<2, 8, 640, true>{}) : f(Build<2, 8, 512, false>{});
+            return table ? f(Build<2, 8, 1024, true>{}) : f(Build<2, 8, 1024, false>{});
         case 4: return table ? f(Build<4, 4, 640, true>{}) : f(Build<4, 4, 512, false>{});
         default: return f(Build<8, 4, 1024, false>{});
     }
