@@ -115,8 +115,34 @@ inline ScoreSpace carve_score(void* base, int32_t B, int32_t T, int32_t N, int32
     return s;
 }
 
-// Workspace of the policy losses: the sums of each row of the batch, then three numbers a frame.
-inline size_t policy_sums_bytes(int32_t B) { return align_up((size_t)B * 4 * sizeof(double), 256); }
+// Sums over what takes part of a row.
+struct PolicySums {
+    double loss, kl, clipped, n;
+};
+
+// One entry: adds to the row's sums and returns the loss's derivative to the log-probability.
+__device__ inline double policy_entry(double l, double l_old, bool has_ref, double l_ref, double A,
+                                      const fltop_policy& p, PolicySums* s) {
+    const double r = exp(l - l_old);
+    const double plain = r * A;
+    const double cut = fmin(fmax(r, 1.0 - p.clip_low), 1.0 + p.clip_high) * A;
+    const double gap = has_ref ? l_ref - l : 0.0;
+    const double e = expm1(gap);
+    const double kl = e - gap;
+    s->loss += fmax(-plain, -cut) + p.kl_weight * kl;
+    s->kl += kl;
+    s->clipped += plain > cut ? 1.0 : 0.0;
+    s->n += 1.0;
+    return (plain <= cut ? -plain : 0.0) - p.kl_weight * e;
+}
+
+
+// Workspace of the policy losses: over given log-probabilities the sums of each row; over logits the frames of each
+// utterance that take part, then three sums from each workgroup.
+inline size_t policy_sums_bytes(int32_t B) { return align_up((size_t)B * sizeof(PolicySums), 256); }
+constexpr int32_t kMostRowGroups = 2048;
+inline size_t row_counts_bytes(int32_t B) { return align_up((size_t)B * sizeof(int32_t), 256); }
+inline size_t row_workspace_bytes(int32_t B) { return row_counts_bytes(B) + 3 * sizeof(double) * kMostRowGroups; }
 
 hipError_t launch_score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores,
                         const ScoreSpace* keep, hipStream_t stream);

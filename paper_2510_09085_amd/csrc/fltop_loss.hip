@@ -108,27 +108,6 @@ __global__ __launch_bounds__(kThreads) void preference_mean_kernel(fltop_prefere
         p.grad_scores[i] *= each * p.scale;
 }
 
-// Sums over what takes part of a row.
-struct PolicySums {
-    double loss, kl, clipped, n;
-};
-
-// One entry: adds to the row's sums and returns the loss's derivative to the log-probability.
-__device__ inline double policy_entry(double l, double l_old, bool has_ref, double l_ref, double A,
-                                      const fltop_policy& p, PolicySums* s) {
-    const double r = exp(l - l_old);
-    const double plain = r * A;
-    const double cut = fmin(fmax(r, 1.0 - p.clip_low), 1.0 + p.clip_high) * A;
-    const double gap = has_ref ? l_ref - l : 0.0;
-    const double e = expm1(gap);
-    const double kl = e - gap;
-    s->loss += fmax(-plain, -cut) + p.kl_weight * kl;
-    s->kl += kl;
-    s->clipped += plain > cut ? 1.0 : 0.0;
-    s->n += 1.0;
-    return (plain <= cut ? -plain : 0.0) - p.kl_weight * e;
-}
-
 __global__ __launch_bounds__(kThreads) void policy_kernel(const double* scores, const double* old_scores,
                                                           const double* ref_scores, const double* advantages,
                                                           const int32_t* counts, int32_t N, fltop_policy p,
@@ -209,112 +188,6 @@ __global__ __launch_bounds__(kThreads) void policy_mean_kernel(const PolicySums*
         grad_scores[i] *= policy_weight(sums[i / N].n, t, p.reduction) * p.scale;
 }
 
-// ---- the policy loss from logits -----------------------------------------------------------------
-
-__global__ __launch_bounds__(kThreads) void part_kernel(fltop_rows x, const int32_t* tokens, PolicySums* sums) {
-    __shared__ double scratch[kThreads / kWave];
-    const int32_t b = blockIdx.x;
-    const int32_t frames = min(x.lengths[b], x.T);
-    double n = 0.0;
-    for (int32_t t = threadIdx.x; t < frames; t += kThreads)
-        n += (uint32_t)tokens[(int64_t)b * x.T + t] < (uint32_t)x.V ? 1.0 : 0.0;
-    n = block_sum(n, scratch);
-    if (threadIdx.x == 0) sums[b] = {0.0, 0.0, 0.0, n};
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void policy_rows_kernel(fltop_rows x, const int32_t* tokens,
-                                                               const float* old_logps, const float* ref_logps,
-                                                               const float* advantages, bool per_frame,
-                                                               fltop_policy p, const PolicySums* counted,
-                                                               double* entries, float* logps, T* grad) {
-    __shared__ double scratch[kThreads / kWave];
-    __shared__ float tops[kThreads / kWave];
-    const PolicyTotal total = policy_total(counted, x.B, p.reduction, scratch);
-    const int64_t rows = (int64_t)x.B * x.T;
-    for (int64_t at = blockIdx.x; at < rows; at += gridDim.x) {
-        const int32_t b = (int32_t)(at / x.T), t = (int32_t)(at % x.T);
-        T* out = grad + at * x.V;
-        const int32_t tok = t < x.lengths[b] ? tokens[at] : -1;
-        if ((uint32_t)tok >= (uint32_t)x.V) {
-            for (int32_t v = threadIdx.x; v < x.V; v += kThreads) out[v] = from_float<T>(0.0f);
-            if (threadIdx.x == 0) {
-                logps[at] = 0.0f;
-                entries[3 * at] = entries[3 * at + 1] = entries[3 * at + 2] = 0.0;
-            }
-            continue;
-        }
-        const T* row = static_cast<const T*>(x.data) + b * x.batch_stride + t * x.frame_stride;
-        float top = -INFINITY;
-        for (int32_t v = threadIdx.x; v < x.V; v += kThreads) top = fmaxf(top, to_float(row[v]));
-#pragma unroll
-        for (int o = kWave / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-        __syncthreads();
-        if ((threadIdx.x & (kWave - 1)) == 0) tops[threadIdx.x / kWave] = top;
-        __syncthreads();
-        for (int w = 0; w < kThreads / kWave; ++w) top = fmaxf(top, tops[w]);
-        // the others' mass apart from the token's own: 1 - p and ln p keep their digits where p is nearly 1
-        float rest = 0.0f;
-        for (int32_t v = threadIdx.x; v < x.V; v += kThreads) rest += v == tok ? 0.0f : expf(to_float(row[v]) - top);
-        const double others = block_sum((double)rest, scratch);
-        const double gap = (double)to_float(row[tok]) - (double)top;
-        const double own = exp(gap);
-        const double sum = others + own;
-        const double l = own > others ? -log1p(others / own) : gap - log(sum);
-        PolicySums s = {0.0, 0.0, 0.0, 0.0};
-        const double A = advantages[per_frame ? at : b];
-        const double d = policy_entry(l, old_logps[at], ref_logps != nullptr, ref_logps ? ref_logps[at] : 0.0, A, p, &s) *
-                         (policy_weight(counted[b].n, total, p.reduction) * p.scale);
-        const float by = (float)(-d / sum);
-        for (int32_t v = threadIdx.x; v < x.V; v += kThreads)
-            out[v] = from_float<T>(v == tok ? (float)(d * (others / sum)) : expf(to_float(row[v]) - top) * by);
-        if (threadIdx.x == 0) {
-            logps[at] = (float)l;
-            entries[3 * at] = s.loss;
-            entries[3 * at + 1] = s.kl;
-            entries[3 * at + 2] = s.clipped;
-        }
-    }
-}
-
-// The frames' losses of each utterance, then of the batch.
-__global__ __launch_bounds__(kThreads) void policy_rows_sum_kernel(int32_t T, const double* entries, PolicySums* sums) {
-    __shared__ double scratch[kThreads / kWave];
-    const int32_t b = blockIdx.x;
-    double s[3] = {0.0, 0.0, 0.0};
-    for (int32_t t = threadIdx.x; t < T; t += kThreads)
-        for (int k = 0; k < 3; ++k) s[k] += entries[3 * ((int64_t)b * T + t) + k];
-    for (int k = 0; k < 3; ++k) s[k] = block_sum(s[k], scratch);
-    if (threadIdx.x == 0) sums[b] = {s[0], s[1], s[2], sums[b].n};
-}
-
-__global__ __launch_bounds__(kThreads) void policy_summary_kernel(const PolicySums* sums, int32_t B, int32_t reduction,
-                                                                  float* summary) {
-    __shared__ double scratch[kThreads / kWave];
-    const PolicyTotal t = policy_total(sums, B, reduction, scratch);
-    if (threadIdx.x == 0) {
-        summary[0] = (float)t.loss;
-        summary[1] = (float)t.kl;
-        summary[2] = (float)t.clipped;
-    }
-}
-
-template <typename T>
-hipError_t policy_rows(const fltop_rows& x, const int32_t* tokens, const float* old_logps, const float* ref_logps,
-                       const float* advantages, bool per_frame, const fltop_policy& policy, void* workspace,
-                       float* summary, float* logps, void* grad, hipStream_t stream) {
-    PolicySums* sums = static_cast<PolicySums*>(workspace);
-    double* entries = reinterpret_cast<double*>(static_cast<char*>(workspace) + policy_sums_bytes(x.B));
-    hipLaunchKernelGGL(part_kernel, dim3(x.B), dim3(kThreads), 0, stream, x, tokens, sums);
-    const int64_t rows = (int64_t)x.B * x.T;
-    hipLaunchKernelGGL(policy_rows_kernel<T>, dim3((unsigned)(rows < 4096 ? rows : 4096)), dim3(kThreads), 0, stream, x,
-                       tokens, old_logps, ref_logps, advantages, per_frame, policy, sums, entries, logps,
-                       static_cast<T*>(grad));
-    hipLaunchKernelGGL(policy_rows_sum_kernel, dim3(x.B), dim3(kThreads), 0, stream, x.T, entries, sums);
-    hipLaunchKernelGGL(policy_summary_kernel, dim3(1), dim3(kThreads), 0, stream, sums, x.B, policy.reduction, summary);
-    return hipGetLastError();
-}
-
 unsigned blocks_for(int64_t n) {
     const int64_t blocks = (n + kThreads - 1) / kThreads;
     return (unsigned)(blocks < 1024 ? blocks : 1024);
@@ -339,20 +212,6 @@ hipError_t launch_policy(const double* scores, const double* old_scores, const d
     hipLaunchKernelGGL(policy_mean_kernel, dim3(blocks_for((int64_t)B * N)), dim3(kThreads), 0, stream, sums, B, N,
                        policy, summary, grad_scores);
     return hipGetLastError();
-}
-
-hipError_t launch_policy_logits(const fltop_rows& x, const int32_t* tokens, const float* old_logps,
-                                const float* ref_logps, const float* advantages, bool per_frame,
-                                const fltop_policy& policy, void* workspace, float* summary, float* logps, void* grad,
-                                hipStream_t stream) {
-    if (x.type == FLTOP_TYPE_BF16)
-        return policy_rows<__hip_bfloat16>(x, tokens, old_logps, ref_logps, advantages, per_frame, policy, workspace,
-                                           summary, logps, grad, stream);
-    if (x.type == FLTOP_TYPE_F16)
-        return policy_rows<__half>(x, tokens, old_logps, ref_logps, advantages, per_frame, policy, workspace, summary,
-                                   logps, grad, stream);
-    return policy_rows<float>(x, tokens, old_logps, ref_logps, advantages, per_frame, policy, workspace, summary, logps,
-                              grad, stream);
 }
 
 }  // namespace fltop

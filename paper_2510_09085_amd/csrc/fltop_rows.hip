@@ -1,0 +1,498 @@
+// The clipped policy loss from logits: for each frame the log-softmax at its token, the loss and its derivative to that
+// log-probability, and from it the gradient of the whole row,
+//     d/dx_v = c ([v = token] - softmax(x)_v),   c = df/dl * weight.
+// Rows are read once and stay in registers between their statistics and their gradient: what bounds these kernels is
+// reading the logits and writing the gradient.
+//
+// Three launches.  Means need the number of frames that take part before any gradient: one kernel counts them for each
+// utterance.  Then the rows; each workgroup adds the counts up, in one order.  The frames' losses are summed lane by lane
+// in a fixed assignment of rows, one sum is left by each workgroup, and the last kernel adds those.
+#include "fltop_learn.h"
+
+namespace fltop {
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kThreads = 256;
+constexpr int kLongThreads = 1024;
+
+template <typename T> constexpr int kVec = 16 / sizeof(T);
+
+// 16 bytes of a row, wherever they lie (gfx950 loads and stores vectors at any address).
+template <typename T>
+struct Vec {
+    T x[kVec<T>];
+    // Makes the compiler take the values for new ones: what it made of them before (floats, exponentials, one or two
+    // registers a value) is worked out again rather than kept in registers next to them.
+    __device__ void renew() {
+        uint32_t w[4];
+        __builtin_memcpy(w, x, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
+        __builtin_memcpy(x, w, 16);
+    }
+};
+template <typename T>
+__device__ inline Vec<T> load_vec(const T* from) {
+    Vec<T> v;
+    __builtin_memcpy(&v, from, 16);
+    return v;
+}
+template <typename T>
+__device__ inline void store_vec(T* to, const Vec<T>& v) { __builtin_memcpy(to, &v, 16); }
+
+// The part of a row that lies behind its last whole vector is moved value by value; places behind it hold -inf.
+template <typename T>
+__device__ inline Vec<T> load_part(const T* row, int32_t at, int32_t V) {
+    if (at + kVec<T> <= V) return load_vec(row + at);
+    Vec<T> v;
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) v.x[e] = at + e < V ? row[at + e] : from_float<T>(-INFINITY);
+    return v;
+}
+template <typename T>
+__device__ inline void store_part(T* row, int32_t at, int32_t V, const Vec<T>& v) {
+    if (at + kVec<T> <= V) {
+        store_vec(row + at, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e)
+        if (at + e < V) row[at + e] = v.x[e];
+}
+
+// exp(x) for x <= 0, within two steps of fp32 and what x * log2(e) is off.
+__device__ inline float exp_down(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+template <int N>
+__device__ inline float max_of(float x) {
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, kWave));
+    return x;
+}
+template <int N>
+__device__ inline float sum_of(float x) {
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
+    return x;
+}
+__device__ inline double sum_of_wave(double x) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
+    return x;
+}
+
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__global__ __launch_bounds__(kThreads) void part_kernel(fltop_rows x, const int32_t* tokens, int32_t* counts) {
+    __shared__ int32_t of_wave[kThreads / kWave];
+    const int32_t b = blockIdx.x;
+    const int32_t frames = min(x.lengths[b], x.T);
+    int32_t n = 0;
+    for (int32_t t = threadIdx.x; t < frames; t += kThreads)
+        n += (uint32_t)tokens[(int64_t)b * x.T + t] < (uint32_t)x.V ? 1 : 0;
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) n += __shfl_xor(n, o, kWave);
+    if (threadIdx.x % kWave == 0) of_wave[threadIdx.x / kWave] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) counts[b] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
+}
+
+// Everything but the logits of a call.
+struct Frames {
+    const int32_t* tokens;
+    const float *old_logps, *ref_logps, *advantages;
+    int32_t per_frame;
+    const int32_t* counts;   // [B]
+    double* partial;         // [workgroups][3]
+    float* logps;
+};
+
+// What a frame's entry weighs: frames that take part, and utterances that have any.
+struct Weights {
+    double all, rows;
+    int32_t reduction;
+    // `scratch`: two numbers for each wavefront
+    __device__ Weights(const int32_t* counts, int32_t B, int32_t how, int64_t* scratch) : reduction(how) {
+        int64_t n = 0, some = 0;
+        for (int32_t b = threadIdx.x; b < B; b += blockDim.x) {
+            n += counts[b];
+            some += counts[b] > 0;
+        }
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) {
+            n += __shfl_xor(n, o, kWave);
+            some += __shfl_xor(some, o, kWave);
+        }
+        const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+        if (threadIdx.x % kWave == 0) {
+            scratch[wave] = n;
+            scratch[waves + wave] = some;
+        }
+        __syncthreads();
+        n = some = 0;
+        for (int w = 0; w < waves; ++w) {
+            n += scratch[w];
+            some += scratch[waves + w];
+        }
+        all = (double)n;
+        rows = (double)some;
+        __syncthreads();
+    }
+    __device__ double of(int32_t count) const {
+        return reduction == FLTOP_REDUCE_TOKEN ? 1.0 / all : reduction == FLTOP_REDUCE_SEQUENCE ? 1.0 / (count * rows) : 1.0;
+    }
+};
+
+struct Sums {
+    double loss = 0.0, kl = 0.0, clipped = 0.0;
+};
+
+// What the row needs of a frame: gradients are e * by for the others' exponentials e, and `own` at the token.
+struct RowGradient {
+    float by, own;
+};
+
+// A frame of a token, from its row's statistics: others = sum of exp(x_v - top) over v other than the token (so that
+// 1 - p and ln p keep their digits where p is nearly 1), gap = x_token - top.  fp64: one frame's worth of it, shared by
+// the whole row.
+__device__ inline RowGradient frame_gradient(const Frames& f, int64_t at, int32_t b, float top, float rest, float x_token,
+                                             const fltop_policy& p, const Weights& weights, Sums* sums) {
+    const double gap = (double)x_token - (double)top, others = rest;
+    const double own = exp(gap), sum = others + own;
+    const double l = own > others ? -log1p(others / own) : gap - log(sum);
+    const double weight = weights.of(f.counts[b]);
+    PolicySums s = {0.0, 0.0, 0.0, 0.0};
+    const double d = policy_entry(l, f.old_logps[at], f.ref_logps != nullptr, f.ref_logps ? f.ref_logps[at] : 0.0,
+                                  f.advantages[f.per_frame ? at : b], p, &s) *
+                     (weight * p.scale);
+    sums->loss += s.loss * weight;
+    sums->kl += s.kl * weight;
+    sums->clipped += s.clipped;
+    f.logps[at] = (float)l;
+    return {(float)(-d / sum), (float)(d * (others / sum))};
+}
+
+// Leaves a workgroup's sums.
+template <int THREADS>
+__device__ inline void leave_sums(const Sums& mine, double* partial) {
+    __shared__ double of_wave[THREADS / kWave][3];
+    const double s[3] = {sum_of_wave(mine.loss), sum_of_wave(mine.kl), sum_of_wave(mine.clipped)};
+    if (threadIdx.x % kWave == 0)
+        for (int k = 0; k < 3; ++k) of_wave[threadIdx.x / kWave][k] = s[k];
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double sum = 0.0;
+        for (int w = 0; w < THREADS / kWave; ++w) sum += of_wave[w][threadIdx.x];
+        partial[3 * (int64_t)blockIdx.x + threadIdx.x] = sum;
+    }
+}
+
+// Short rows: LANES lanes take a row, ITER vectors each, and a wavefront PASSES times kWave / LANES rows before it goes on
+// to their losses, for which each row has a lane of its own: that arithmetic, in fp64 a few hundred instructions, is done
+// once for all of them.
+template <typename T, int LANES, int ITER, int PASSES>
+__global__ __launch_bounds__(kThreads) void short_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
+    constexpr int kAtOnce = kWave / LANES, kRows = kAtOnce * PASSES, N = kVec<T>;
+    static_assert(kRows <= kWave, "a lane for each row");
+    struct Row {
+        int64_t start;   // of its logits
+        int32_t token;   // -1: takes no part
+        float top, rest, x_token;
+        RowGradient g;
+    };
+    __shared__ Row rows_of[kThreads / kWave][kRows];
+    __shared__ int64_t scratch[2 * kThreads / kWave];
+    const Weights weights(f.counts, x.B, p.reduction, scratch);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int group = lane / LANES, within = lane % LANES;
+    Row* const rows = rows_of[wave];
+    const int64_t total = (int64_t)x.B * x.T, step = (int64_t)gridDim.x * (kThreads / kWave) * kRows;
+    const T* const data = static_cast<const T*>(x.data);
+    Sums sums;
+    for (int64_t first = ((int64_t)blockIdx.x * (kThreads / kWave) + wave) * kRows; first < total; first += step) {
+        const int64_t at = first + lane;
+        int32_t b = 0, token = -1;
+        if (lane < kRows) {
+            if (at < total) {
+                b = (int32_t)((uint32_t)at / (uint32_t)x.T);
+                const int32_t t = (int32_t)at - b * x.T;
+                if (t < x.lengths[b]) token = f.tokens[at];
+                if ((uint32_t)token >= (uint32_t)x.V) token = -1;
+                rows[lane].start = b * x.batch_stride + t * x.frame_stride;
+            }
+            rows[lane].token = token;
+        }
+        wave_fence();
+        Vec<T> v[PASSES][ITER];
+#pragma unroll
+        for (int s = 0; s < PASSES; ++s) {
+            const Row& row = rows[s * kAtOnce + group];
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+                const int32_t c = (i * LANES + within) * N;
+                if (row.token >= 0 && c < x.V) {
+                    v[s][i] = load_part(data + row.start, c, x.V);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[s][i].x[e] = from_float<T>(-INFINITY);
+                }
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < PASSES; ++s) {
+            Row& row = rows[s * kAtOnce + group];
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) top = fmaxf(top, to_float(v[s][i].x[e]));
+            top = max_of<LANES>(top);
+            float rest = 0.0f;
+#pragma unroll
+            for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int32_t c = (i * LANES + within) * N + e;
+                    const float y = to_float(v[s][i].x[e]);
+                    if (c == row.token) row.x_token = y;
+                    rest += c == row.token || c >= x.V ? 0.0f : exp_down(y - top);
+                }
+            rest = sum_of<LANES>(rest);
+            if (within == 0) {
+                row.top = top;
+                row.rest = rest;
+            }
+        }
+        wave_fence();
+#pragma unroll
+        for (int s = 0; s < PASSES; ++s)
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) v[s][i].renew();
+        if (token >= 0)
+            rows[lane].g = frame_gradient(f, at, b, rows[lane].top, rows[lane].rest, rows[lane].x_token, p, weights, &sums);
+        else if (lane < kRows && at < total)
+            f.logps[at] = 0.0f;
+        wave_fence();
+#pragma unroll
+        for (int s = 0; s < PASSES; ++s) {
+            const int r = s * kAtOnce + group;
+            const Row& row = rows[r];
+            if (first + r >= total) continue;
+            T* const out = grad + (first + r) * x.V;
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+                const int32_t c = (i * LANES + within) * N;
+                if (c >= x.V) continue;
+                Vec<T> g;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float one = c + e == row.token ? row.g.own : exp_down(to_float(v[s][i].x[e]) - row.top) * row.g.by;
+                    g.x[e] = from_float<T>(row.token >= 0 ? one : 0.0f);
+                }
+                store_part(out, c, x.V, g);
+            }
+        }
+        wave_fence();
+    }
+    leave_sums<kThreads>(sums, f.partial);
+}
+
+// Long rows: a workgroup for each.  With HELD the row's vectors stay in registers; rows beyond what THREADS hold are read
+// again for their gradient.
+template <typename T, int THREADS, int ITER, bool HELD>
+__global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
+    constexpr int N = kVec<T>, kWaves = THREADS / kWave;
+    __shared__ int64_t scratch[2 * kWaves];
+    __shared__ float tops[kWaves], rests[kWaves];
+    __shared__ RowGradient shared_g;
+    const Weights weights(f.counts, x.B, p.reduction, scratch);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t total = (int64_t)x.B * x.T;
+    Sums sums;
+    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+        const int32_t b = (int32_t)((uint32_t)at / (uint32_t)x.T), t = (int32_t)at - b * x.T;
+        const int32_t token = t < x.lengths[b] ? f.tokens[at] : -1;
+        T* const out = grad + at * x.V;
+        if ((uint32_t)token >= (uint32_t)x.V) {
+            Vec<T> zero;
+#pragma unroll
+            for (int e = 0; e < N; ++e) zero.x[e] = from_float<T>(0.0f);
+            for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) store_part(out, c, x.V, zero);
+            if (threadIdx.x == 0) f.logps[at] = 0.0f;
+            continue;
+        }
+        const T* const row = static_cast<const T*>(x.data) + b * x.batch_stride + t * x.frame_stride;
+        const float x_token = to_float(row[token]);
+        Vec<T> v[HELD ? ITER : 1];
+        // this lane's own maximum and sum; lanes are put together afterwards
+        float top = -INFINITY, rest = 0.0f;
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+                const int32_t c = (i * THREADS + (int)threadIdx.x) * N;
+                if (c < x.V) {
+                    v[i] = load_part(row, c, x.V);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[i].x[e] = from_float<T>(-INFINITY);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) top = fmaxf(top, to_float(v[i].x[e]));
+            top = max_of<kWave>(top);
+            if (lane == 0) tops[wave] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) v[i].renew();
+#pragma unroll
+            for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int32_t c = (i * THREADS + (int)threadIdx.x) * N + e;
+                    rest += c == token || c >= x.V ? 0.0f : exp_down(to_float(v[i].x[e]) - top);
+                }
+        } else {
+            for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) {
+                const Vec<T> one = load_part(row, c, x.V);
+                float m = top;
+#pragma unroll
+                for (int e = 0; e < N; ++e) m = fmaxf(m, to_float(one.x[e]));
+                if (m > top) {   // the sum so far is rescaled
+                    rest *= exp_down(top - m);
+                    top = m;
+                }
+                if (top > -INFINITY) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) rest += c + e == token || c + e >= x.V ? 0.0f : exp_down(to_float(one.x[e]) - top);
+                }
+            }
+            const float mine = top;
+            top = max_of<kWave>(top);
+            if (lane == 0) tops[wave] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+            if (mine < top) rest *= exp_down(mine - top);
+        }
+        rest = sum_of<kWave>(rest);
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) v[i].renew();
+        }
+        if (lane == 0) rests[wave] = rest;
+        __syncthreads();
+        if (wave == 0) {
+            float all = lane < kWaves ? rests[lane] : 0.0f;
+            all = sum_of<kWave>(all);
+            if (lane == 0) shared_g = frame_gradient(f, at, b, top, all, x_token, p, weights, &sums);
+        }
+        __syncthreads();
+        const RowGradient g = shared_g;
+        auto give = [&](const Vec<T>& one, int32_t c) {
+            Vec<T> o;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                o.x[e] = from_float<T>(c + e == token ? g.own : exp_down(to_float(one.x[e]) - top) * g.by);
+            store_part(out, c, x.V, o);
+        };
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+                const int32_t c = (i * THREADS + (int)threadIdx.x) * N;
+                if (c < x.V) give(v[i], c);
+            }
+        } else {
+            for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) give(load_part(row, c, x.V), c);
+        }
+    }
+    leave_sums<THREADS>(sums, f.partial);
+}
+
+__global__ __launch_bounds__(kLongThreads) void policy_summary_kernel(const int32_t* counts, int32_t B, int32_t reduction,
+                                                                      const double* partial, int32_t groups, float* summary) {
+    __shared__ int64_t scratch[2 * kLongThreads / kWave];
+    __shared__ double of_wave[kLongThreads / kWave][3];
+    const Weights weights(counts, B, reduction, scratch);
+    Sums s;
+    for (int32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+        s.loss += partial[3 * g];
+        s.kl += partial[3 * g + 1];
+        s.clipped += partial[3 * g + 2];
+    }
+    const double mine[3] = {sum_of_wave(s.loss), sum_of_wave(s.kl), sum_of_wave(s.clipped)};
+    if (threadIdx.x % kWave == 0)
+        for (int k = 0; k < 3; ++k) of_wave[threadIdx.x / kWave][k] = mine[k];
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double sum = 0.0;
+        for (int w = 0; w < kLongThreads / kWave; ++w) sum += of_wave[w][threadIdx.x];
+        if (threadIdx.x == 2) sum = weights.all > 0.0 ? sum / weights.all : 0.0;
+        summary[threadIdx.x] = (float)sum;
+    }
+}
+
+template <typename T, int LANES, int ITER, int PASSES>
+int32_t short_rows(const fltop_rows& x, const Frames& f, const fltop_policy& p, void* grad, hipStream_t stream) {
+    const int64_t rows = (int64_t)x.B * x.T, each = (int64_t)(kThreads / kWave) * (kWave / LANES) * PASSES;
+    int64_t groups = (rows + each - 1) / each;
+    if (groups > kMostRowGroups) groups = kMostRowGroups;
+    hipLaunchKernelGGL((short_rows_kernel<T, LANES, ITER, PASSES>), dim3((unsigned)groups), dim3(kThreads), 0, stream, x, f, p,
+                       static_cast<T*>(grad));
+    return (int32_t)groups;
+}
+
+template <typename T, int THREADS, int ITER, bool HELD>
+int32_t long_rows(const fltop_rows& x, const Frames& f, const fltop_policy& p, void* grad, hipStream_t stream) {
+    const int64_t rows = (int64_t)x.B * x.T;
+    const int32_t groups = (int32_t)(rows < kMostRowGroups ? rows : kMostRowGroups);
+    hipLaunchKernelGGL((long_rows_kernel<T, THREADS, ITER, HELD>), dim3(groups), dim3(THREADS), 0, stream, x, f, p,
+                       static_cast<T*>(grad));
+    return groups;
+}
+
+// As few lanes as hold a row in one vector each, up to a wavefront; then as few vectors as a wavefront, a workgroup of
+// 256 and one of 1024 hold it in.
+template <typename T>
+int32_t rows_of(const fltop_rows& x, const Frames& f, const fltop_policy& p, void* grad, hipStream_t stream) {
+    const int32_t vectors = (x.V + kVec<T> - 1) / kVec<T>;
+    if (vectors <= 4) return short_rows<T, 4, 1, 4>(x, f, p, grad, stream);
+    if (vectors <= 8) return short_rows<T, 8, 1, 8>(x, f, p, grad, stream);
+    if (vectors <= 16) return short_rows<T, 16, 1, 8>(x, f, p, grad, stream);
+    if (vectors <= 32) return short_rows<T, 32, 1, 8>(x, f, p, grad, stream);
+    if (vectors <= 64) return short_rows<T, 64, 1, 8>(x, f, p, grad, stream);
+    if (vectors <= 128) return short_rows<T, 64, 2, 4>(x, f, p, grad, stream);
+    if (vectors <= 256) return short_rows<T, 64, 4, 2>(x, f, p, grad, stream);
+    if (vectors <= 1024) return long_rows<T, 256, 4, true>(x, f, p, grad, stream);
+    if (vectors <= 2048) return long_rows<T, 256, 8, true>(x, f, p, grad, stream);
+    if (vectors <= 4096) return long_rows<T, 1024, 4, true>(x, f, p, grad, stream);
+    if (vectors <= 8192) return long_rows<T, 1024, 8, true>(x, f, p, grad, stream);
+    return long_rows<T, 1024, 1, false>(x, f, p, grad, stream);
+}
+
+}  // namespace
+
+hipError_t launch_policy_logits(const fltop_rows& x, const int32_t* tokens, const float* old_logps,
+                                const float* ref_logps, const float* advantages, bool per_frame,
+                                const fltop_policy& policy, void* workspace, float* summary, float* logps, void* grad,
+                                hipStream_t stream) {
+    int32_t* const counts = static_cast<int32_t*>(workspace);
+    double* const partial = reinterpret_cast<double*>(static_cast<char*>(workspace) + row_counts_bytes(x.B));
+    hipLaunchKernelGGL(part_kernel, dim3(x.B), dim3(kThreads), 0, stream, x, tokens, counts);
+    const Frames f = {tokens, old_logps, ref_logps, advantages, per_frame, counts, partial, logps};
+    const int32_t groups = x.type == FLTOP_TYPE_BF16  ? rows_of<__hip_bfloat16>(x, f, policy, grad, stream)
+                           : x.type == FLTOP_TYPE_F16 ? rows_of<__half>(x, f, policy, grad, stream)
+                                                      : rows_of<float>(x, f, policy, grad, stream);
+    hipLaunchKernelGGL(policy_summary_kernel, dim3(1), dim3(kLongThreads), 0, stream, counts, x.B, policy.reduction, partial,
+                       groups, summary);
+    return hipGetLastError();
+}
+
+}  // namespace fltop
