@@ -41,6 +41,30 @@ __device__ inline Vec<T> load_vec(const T* from) {
 template <typename T>
 __device__ inline void store_vec(T* to, const Vec<T>& v) { __builtin_memcpy(to, &v, 16); }
 
+// Rounds a vector's values from fp32, two by two where the type has an instruction for that.
+typedef float Float2 __attribute__((ext_vector_type(2)));
+typedef __bf16 Bf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
+__device__ inline Vec<float> rounded(const float (&f)[4], const float*) {
+    Vec<float> v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v.x[e] = f[e];
+    return v;
+}
+template <typename Pair, typename T>
+__device__ inline Vec<T> rounded_pairs(const float (&f)[8]) {
+    Pair p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = __builtin_convertvector((Float2){f[2 * e], f[2 * e + 1]}, Pair);
+    Vec<T> v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+__device__ inline Vec<__hip_bfloat16> rounded(const float (&f)[8], const __hip_bfloat16*) {
+    return rounded_pairs<Bf2, __hip_bfloat16>(f);
+}
+__device__ inline Vec<__half> rounded(const float (&f)[8], const __half*) { return rounded_pairs<Half2, __half>(f); }
+
 // The part of a row that lies behind its last whole vector is moved value by value; places behind it hold -inf.
 template <typename T>
 __device__ inline Vec<T> load_part(const T* row, int32_t at, int32_t V) {
@@ -59,6 +83,19 @@ __device__ inline void store_part(T* row, int32_t at, int32_t V, const Vec<T>& v
 #pragma unroll
     for (int e = 0; e < kVec<T>; ++e)
         if (at + e < V) row[at + e] = v.x[e];
+}
+
+// Takes the token out of a lane's vector that starts at c (its place then has no mass); whether it was there.
+template <typename T>
+__device__ inline bool take_token(Vec<T>& v, int32_t c, int32_t token, float* x_token) {
+    if ((uint32_t)(token - c) >= (uint32_t)kVec<T>) return false;
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) {
+        if (c + e != token) continue;
+        *x_token = to_float(v.x[e]);
+        v.x[e] = from_float<T>(-INFINITY);
+    }
+    return true;
 }
 
 // exp(x) for x <= 0, within two steps of fp32 and what x * log2(e) is off.
@@ -156,24 +193,40 @@ struct RowGradient {
     float by, own;
 };
 
-// A frame of a token, from its row's statistics: others = sum of exp(x_v - top) over v other than the token (so that
-// 1 - p and ln p keep their digits where p is nearly 1), gap = x_token - top.  fp64: one frame's worth of it, shared by
-// the whole row.
+// exp(x) - x - 1 with its digits where x is small: x^2 (1/2 + x/6 + .. + x^6/40320) leaves out x^9/9!, below 2^-27 of it.
+__device__ inline float exp_beyond_line(float x) {
+    if (fabsf(x) > 0.5f) return expm1f(x) - x;
+    float p = 1.0f / 40320.0f;
+    p = fmaf(p, x, 1.0f / 5040.0f);
+    p = fmaf(p, x, 1.0f / 720.0f);
+    p = fmaf(p, x, 1.0f / 120.0f);
+    p = fmaf(p, x, 1.0f / 24.0f);
+    p = fmaf(p, x, 1.0f / 6.0f);
+    p = fmaf(p, x, 0.5f);
+    return p * x * x;
+}
+
+// A frame of a token, from its row's statistics: rest = sum of exp(x_v - top) over v other than the token (so that 1 - p
+// and ln p keep their digits where p is nearly 1).  Exponentials and logarithms are fp32, as the statistics are; the
+// log-probability they make and its differences are taken in fp64, sums of frames too.
 __device__ inline RowGradient frame_gradient(const Frames& f, int64_t at, int32_t b, float top, float rest, float x_token,
                                              const fltop_policy& p, const Weights& weights, Sums* sums) {
-    const double gap = (double)x_token - (double)top, others = rest;
-    const double own = exp(gap), sum = others + own;
-    const double l = own > others ? -log1p(others / own) : gap - log(sum);
+    const float gap = x_token - top, own = expf(gap), sum = rest + own;
+    const double l = own > rest ? -(double)log1pf(rest / own) : (double)gap - (double)logf(sum);
     const double weight = weights.of(f.counts[b]);
-    PolicySums s = {0.0, 0.0, 0.0, 0.0};
-    const double d = policy_entry(l, f.old_logps[at], f.ref_logps != nullptr, f.ref_logps ? f.ref_logps[at] : 0.0,
-                                  f.advantages[f.per_frame ? at : b], p, &s) *
-                     (weight * p.scale);
-    sums->loss += s.loss * weight;
-    sums->kl += s.kl * weight;
-    sums->clipped += s.clipped;
+    const float A = f.advantages[f.per_frame ? at : b];
+    const float r = expf((float)(l - f.old_logps[at]));
+    const float cut_r = fminf(fmaxf(r, (float)(1.0 - p.clip_low)), (float)(1.0 + p.clip_high));
+    const float plain = r * A, cut = cut_r * A;
+    const float beyond = f.ref_logps ? (float)(f.ref_logps[at] - l) : 0.0f;
+    const float kl = exp_beyond_line(beyond);
+    const double d = (plain <= cut ? -(double)plain : 0.0) - p.kl_weight * ((double)kl + beyond);
+    sums->loss += (fmaxf(-plain, -cut) + p.kl_weight * kl) * weight;
+    sums->kl += kl * weight;
+    sums->clipped += plain > cut ? 1.0 : 0.0;
     f.logps[at] = (float)l;
-    return {(float)(-d / sum), (float)(d * (others / sum))};
+    const float c = (float)(d * (weight * p.scale));
+    return {-c / sum, c * (rest / sum)};
 }
 
 // Leaves a workgroup's sums.
@@ -195,7 +248,7 @@ __device__ inline void leave_sums(const Sums& mine, double* partial) {
 // to their losses, for which each row has a lane of its own: that arithmetic, in fp64 a few hundred instructions, is done
 // once for all of them.
 template <typename T, int LANES, int ITER, int PASSES>
-__global__ __launch_bounds__(kThreads) void short_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
+__global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
     constexpr int kAtOnce = kWave / LANES, kRows = kAtOnce * PASSES, N = kVec<T>;
     static_assert(kRows <= kWave, "a lane for each row");
     struct Row {
@@ -245,7 +298,13 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(fltop_rows x, Fram
 #pragma unroll
         for (int s = 0; s < PASSES; ++s) {
             Row& row = rows[s * kAtOnce + group];
+            const int32_t tok = row.token;
             float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+                float x_token;
+                if (take_token(v[s][i], (i * LANES + within) * N, tok, &x_token)) row.x_token = top = x_token;
+            }
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
@@ -255,12 +314,7 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(fltop_rows x, Fram
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const int32_t c = (i * LANES + within) * N + e;
-                    const float y = to_float(v[s][i].x[e]);
-                    if (c == row.token) row.x_token = y;
-                    rest += c == row.token || c >= x.V ? 0.0f : exp_down(y - top);
-                }
+                for (int e = 0; e < N; ++e) rest += exp_down(to_float(v[s][i].x[e]) - top);
             rest = sum_of<LANES>(rest);
             if (within == 0) {
                 row.top = top;
@@ -283,17 +337,18 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(fltop_rows x, Fram
             const Row& row = rows[r];
             if (first + r >= total) continue;
             T* const out = grad + (first + r) * x.V;
+            const int32_t tok = row.token;
+            const float top = row.top, by = row.g.by;
 #pragma unroll
             for (int i = 0; i < ITER; ++i) {
                 const int32_t c = (i * LANES + within) * N;
                 if (c >= x.V) continue;
-                Vec<T> g;
+                float g[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float one = c + e == row.token ? row.g.own : exp_down(to_float(v[s][i].x[e]) - row.top) * row.g.by;
-                    g.x[e] = from_float<T>(row.token >= 0 ? one : 0.0f);
-                }
-                store_part(out, c, x.V, g);
+                for (int e = 0; e < N; ++e) g[e] = tok >= 0 ? exp_down(to_float(v[s][i].x[e]) - top) * by : 0.0f;
+                store_part(out, c, x.V, rounded(g, out));
+                // (a wavefront's stores to one place come in their order)
+                if ((uint32_t)(tok - c) < (uint32_t)N) out[tok] = from_float<T>(row.g.own);
             }
         }
         wave_fence();
@@ -327,15 +382,17 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
         }
         const T* const row = static_cast<const T*>(x.data) + b * x.batch_stride + t * x.frame_stride;
         const float x_token = to_float(row[token]);
+        float taken;
         Vec<T> v[HELD ? ITER : 1];
         // this lane's own maximum and sum; lanes are put together afterwards
-        float top = -INFINITY, rest = 0.0f;
+        float top = x_token, rest = 0.0f;
         if constexpr (HELD) {
 #pragma unroll
             for (int i = 0; i < ITER; ++i) {
                 const int32_t c = (i * THREADS + (int)threadIdx.x) * N;
                 if (c < x.V) {
                     v[i] = load_part(row, c, x.V);
+                    take_token(v[i], c, token, &taken);
                 } else {
 #pragma unroll
                     for (int e = 0; e < N; ++e) v[i].x[e] = from_float<T>(-INFINITY);
@@ -355,13 +412,11 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const int32_t c = (i * THREADS + (int)threadIdx.x) * N + e;
-                    rest += c == token || c >= x.V ? 0.0f : exp_down(to_float(v[i].x[e]) - top);
-                }
+                for (int e = 0; e < N; ++e) rest += exp_down(to_float(v[i].x[e]) - top);
         } else {
             for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) {
-                const Vec<T> one = load_part(row, c, x.V);
+                Vec<T> one = load_part(row, c, x.V);
+                take_token(one, c, token, &taken);
                 float m = top;
 #pragma unroll
                 for (int e = 0; e < N; ++e) m = fmaxf(m, to_float(one.x[e]));
@@ -371,7 +426,7 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
                 }
                 if (top > -INFINITY) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) rest += c + e == token || c + e >= x.V ? 0.0f : exp_down(to_float(one.x[e]) - top);
+                    for (int e = 0; e < N; ++e) rest += exp_down(to_float(one.x[e]) - top);
                 }
             }
             const float mine = top;
@@ -397,11 +452,11 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
         __syncthreads();
         const RowGradient g = shared_g;
         auto give = [&](const Vec<T>& one, int32_t c) {
-            Vec<T> o;
+            float o[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                o.x[e] = from_float<T>(c + e == token ? g.own : exp_down(to_float(one.x[e]) - top) * g.by);
-            store_part(out, c, x.V, o);
+            for (int e = 0; e < N; ++e) o[e] = exp_down(to_float(one.x[e]) - top) * g.by;
+            store_part(out, c, x.V, rounded(o, out));
+            if ((uint32_t)(token - c) < (uint32_t)N) out[token] = from_float<T>(g.own);
         };
         if constexpr (HELD) {
 #pragma unroll
