@@ -7,6 +7,8 @@
 // Three launches.  Means need the number of frames that take part before any gradient: one kernel counts them for each
 // utterance.  Then the rows; each workgroup adds the counts up, in one order.  The frames' losses are summed lane by lane
 // in a fixed assignment of rows, one sum is left by each workgroup, and the last kernel adds those.
+#include <type_traits>
+
 #include "fltop_learn.h"
 
 namespace fltop {
@@ -18,71 +20,89 @@ constexpr int kLongThreads = 1024;
 
 template <typename T> constexpr int kVec = 16 / sizeof(T);
 
-// 16 bytes of a row, wherever they lie (gfx950 loads and stores vectors at any address).
-template <typename T>
-struct Vec {
-    T x[kVec<T>];
-    // Makes the compiler take the values for new ones: what it made of them before (floats, exponentials, one or two
-    // registers a value) is worked out again rather than kept in registers next to them.
-    __device__ void renew() {
-        uint32_t w[4];
-        __builtin_memcpy(w, x, 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
-        __builtin_memcpy(x, w, 16);
-    }
-};
-template <typename T>
-__device__ inline Vec<T> load_vec(const T* from) {
-    Vec<T> v;
-    __builtin_memcpy(&v, from, 16);
-    return v;
-}
-template <typename T>
-__device__ inline void store_vec(T* to, const Vec<T>& v) { __builtin_memcpy(to, &v, 16); }
-
-// Rounds a vector's values from fp32, two by two where the type has an instruction for that.
 typedef float Float2 __attribute__((ext_vector_type(2)));
 typedef __bf16 Bf2 __attribute__((ext_vector_type(2)));
 typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
-__device__ inline Vec<float> rounded(const float (&f)[4], const float*) {
-    Vec<float> v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v.x[e] = f[e];
-    return v;
-}
-template <typename Pair, typename T>
-__device__ inline Vec<T> rounded_pairs(const float (&f)[8]) {
-    Pair p[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) p[e] = __builtin_convertvector((Float2){f[2 * e], f[2 * e + 1]}, Pair);
-    Vec<T> v;
-    __builtin_memcpy(&v, p, 16);
-    return v;
-}
-__device__ inline Vec<__hip_bfloat16> rounded(const float (&f)[8], const __hip_bfloat16*) {
-    return rounded_pairs<Bf2, __hip_bfloat16>(f);
-}
-__device__ inline Vec<__half> rounded(const float (&f)[8], const __half*) { return rounded_pairs<Half2, __half>(f); }
 
-// The part of a row that lies behind its last whole vector is moved value by value; places behind it hold -inf.
+// 16 bytes of a row, as they lie in memory: two values of 16 bits in one register.
+template <typename T>
+struct Vec {
+    static constexpr int N = kVec<T>;
+    uint32_t w[4];
+
+    __device__ float operator[](int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        const uint32_t x = w[e / 2];
+        if constexpr (std::is_same<T, __hip_bfloat16>::value) return __uint_as_float(e & 1 ? x & 0xFFFF0000u : x << 16);
+        return __half2float(__ushort_as_half((unsigned short)(e & 1 ? x >> 16 : x)));
+    }
+    static __device__ uint32_t bits(T x) {
+        if constexpr (sizeof(T) == 4) return __float_as_uint(x);
+        unsigned short u;
+        __builtin_memcpy(&u, &x, 2);
+        return u;
+    }
+    __device__ void set(int e, uint32_t bits) {
+        if constexpr (sizeof(T) == 4)
+            w[e] = bits;
+        else
+            w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | bits << 16 : (w[e / 2] & 0xFFFF0000u) | bits;
+    }
+    static __device__ uint32_t no_mass() { return bits(from_float<T>(-INFINITY)); }
+    __device__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? no_mass() : no_mass() << 16 | no_mass();
+    }
+    // Rounds fp32 values, two by two where the type has an instruction for that.
+    __device__ void round(const float (&f)[N]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = __float_as_uint(f[i]);
+            } else if constexpr (std::is_same<T, __hip_bfloat16>::value) {
+                const Bf2 p = __builtin_convertvector((Float2){f[2 * i], f[2 * i + 1]}, Bf2);
+                __builtin_memcpy(&w[i], &p, 4);
+            } else {
+                const Half2 p = __builtin_convertvector((Float2){f[2 * i], f[2 * i + 1]}, Half2);
+                __builtin_memcpy(&w[i], &p, 4);
+            }
+        }
+    }
+    // Makes the compiler take the values for new ones: what it made of them before (floats, exponentials, one or two
+    // registers a value) is worked out again rather than kept in registers next to them.
+    __device__ void renew() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));
+    }
+};
+
+// A row's vectors are loaded and stored wherever they lie (gfx950 does so at any address); the part behind the last whole
+// one is moved value by value, and places behind it hold -inf.
 template <typename T>
 __device__ inline Vec<T> load_part(const T* row, int32_t at, int32_t V) {
-    if (at + kVec<T> <= V) return load_vec(row + at);
     Vec<T> v;
+    if (at + kVec<T> <= V) {
+        __builtin_memcpy(v.w, row + at, 16);
+        return v;
+    }
+    v.clear();
 #pragma unroll
-    for (int e = 0; e < kVec<T>; ++e) v.x[e] = at + e < V ? row[at + e] : from_float<T>(-INFINITY);
+    for (int e = 0; e < kVec<T> - 1; ++e)
+        if (at + e < V) v.set(e, Vec<T>::bits(row[at + e]));
     return v;
 }
 template <typename T>
 __device__ inline void store_part(T* row, int32_t at, int32_t V, const Vec<T>& v) {
     if (at + kVec<T> <= V) {
-        store_vec(row + at, v);
+        __builtin_memcpy(row + at, v.w, 16);
         return;
     }
 #pragma unroll
-    for (int e = 0; e < kVec<T>; ++e)
-        if (at + e < V) row[at + e] = v.x[e];
+    for (int e = 0; e < kVec<T> - 1; ++e)
+        if (at + e < V) {
+            const uint32_t x = sizeof(T) == 4 ? v.w[e] : v.w[e / 2] >> (e & 1 ? 16 : 0);
+            __builtin_memcpy(row + at + e, &x, sizeof(T));
+        }
 }
 
 // Takes the token out of a lane's vector that starts at c (its place then has no mass); whether it was there.
@@ -92,8 +112,8 @@ __device__ inline bool take_token(Vec<T>& v, int32_t c, int32_t token, float* x_
 #pragma unroll
     for (int e = 0; e < kVec<T>; ++e) {
         if (c + e != token) continue;
-        *x_token = to_float(v.x[e]);
-        v.x[e] = from_float<T>(-INFINITY);
+        *x_token = v[e];
+        v.set(e, Vec<T>::no_mass());
     }
     return true;
 }
@@ -290,8 +310,7 @@ __global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, F
                 if (row.token >= 0 && c < x.V) {
                     v[s][i] = load_part(data + row.start, c, x.V);
                 } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) v[s][i].x[e] = from_float<T>(-INFINITY);
+                    v[s][i].clear();
                 }
             }
         }
@@ -308,13 +327,13 @@ __global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, F
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) top = fmaxf(top, to_float(v[s][i].x[e]));
+                for (int e = 0; e < N; ++e) top = fmaxf(top, v[s][i][e]);
             top = max_of<LANES>(top);
             float rest = 0.0f;
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) rest += exp_down(to_float(v[s][i].x[e]) - top);
+                for (int e = 0; e < N; ++e) rest += exp_down(v[s][i][e] - top);
             rest = sum_of<LANES>(rest);
             if (within == 0) {
                 row.top = top;
@@ -345,8 +364,10 @@ __global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, F
                 if (c >= x.V) continue;
                 float g[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) g[e] = tok >= 0 ? exp_down(to_float(v[s][i].x[e]) - top) * by : 0.0f;
-                store_part(out, c, x.V, rounded(g, out));
+                for (int e = 0; e < N; ++e) g[e] = tok >= 0 ? exp_down(v[s][i][e] - top) * by : 0.0f;
+                Vec<T> o;
+                o.round(g);
+                store_part(out, c, x.V, o);
                 // (a wavefront's stores to one place come in their order)
                 if ((uint32_t)(tok - c) < (uint32_t)N) out[tok] = from_float<T>(row.g.own);
             }
@@ -373,9 +394,7 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
         const int32_t token = t < x.lengths[b] ? f.tokens[at] : -1;
         T* const out = grad + at * x.V;
         if ((uint32_t)token >= (uint32_t)x.V) {
-            Vec<T> zero;
-#pragma unroll
-            for (int e = 0; e < N; ++e) zero.x[e] = from_float<T>(0.0f);
+            const Vec<T> zero = {{0, 0, 0, 0}};
             for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) store_part(out, c, x.V, zero);
             if (threadIdx.x == 0) f.logps[at] = 0.0f;
             continue;
@@ -394,14 +413,13 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
                     v[i] = load_part(row, c, x.V);
                     take_token(v[i], c, token, &taken);
                 } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) v[i].x[e] = from_float<T>(-INFINITY);
+                    v[i].clear();
                 }
             }
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) top = fmaxf(top, to_float(v[i].x[e]));
+                for (int e = 0; e < N; ++e) top = fmaxf(top, v[i][e]);
             top = max_of<kWave>(top);
             if (lane == 0) tops[wave] = top;
             __syncthreads();
@@ -412,21 +430,21 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
 #pragma unroll
             for (int i = 0; i < ITER; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) rest += exp_down(to_float(v[i].x[e]) - top);
+                for (int e = 0; e < N; ++e) rest += exp_down(v[i][e] - top);
         } else {
             for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) {
                 Vec<T> one = load_part(row, c, x.V);
                 take_token(one, c, token, &taken);
                 float m = top;
 #pragma unroll
-                for (int e = 0; e < N; ++e) m = fmaxf(m, to_float(one.x[e]));
+                for (int e = 0; e < N; ++e) m = fmaxf(m, one[e]);
                 if (m > top) {   // the sum so far is rescaled
                     rest *= exp_down(top - m);
                     top = m;
                 }
                 if (top > -INFINITY) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) rest += exp_down(to_float(one.x[e]) - top);
+                    for (int e = 0; e < N; ++e) rest += exp_down(one[e] - top);
                 }
             }
             const float mine = top;
@@ -454,8 +472,10 @@ __global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames
         auto give = [&](const Vec<T>& one, int32_t c) {
             float o[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = exp_down(to_float(one.x[e]) - top) * g.by;
-            store_part(out, c, x.V, rounded(o, out));
+            for (int e = 0; e < N; ++e) o[e] = exp_down(one[e] - top) * g.by;
+            Vec<T> rounded;
+            rounded.round(o);
+            store_part(out, c, x.V, rounded);
             if ((uint32_t)(token - c) < (uint32_t)N) out[token] = from_float<T>(g.own);
         };
         if constexpr (HELD) {
