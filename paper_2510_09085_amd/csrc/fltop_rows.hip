@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, F
 // Long rows: a workgroup for each.  With HELD the row's vectors stay in registers; rows beyond what THREADS hold are read
 // again for their gradient.
 template <typename T, int THREADS, int ITER, bool HELD>
-__global__ __launch_bounds__(THREADS) void long_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
+__global__ __launch_bounds__(THREADS, 4) void long_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
     constexpr int N = kVec<T>, kWaves = THREADS / kWave;
     __shared__ int64_t scratch[2 * kWaves];
     __shared__ float tops[kWaves], rests[kWaves];
@@ -547,8 +547,8 @@ int32_t rows_of(const fltop_rows& x, const Frames& f, const fltop_policy& p, voi
     if (vectors <= 256) return short_rows<T, 64, 4, 2>(x, f, p, grad, stream);
     if (vectors <= 1024) return long_rows<T, 256, 4, true>(x, f, p, grad, stream);
     if (vectors <= 2048) return long_rows<T, 256, 8, true>(x, f, p, grad, stream);
-    if (vectors <= 4096) return long_rows<T, 1024, 4, true>(x, f, p, grad, stream);
-    if (vectors <= 8192) return long_rows<T, 1024, 8, true>(x, f, p, grad, stream);
+    if (vectors <= 4096) return long_rows<T, 512, 8, true>(x, f, p, grad, stream);
+    if (vectors <= 8192) return long_rows<T, 512, 16, true>(x, f, p, grad, stream);
     return long_rows<T, 1024, 1, false>(x, f, p, grad, stream);
 }
 
