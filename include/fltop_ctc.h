@@ -359,7 +359,7 @@ int fltop_ctc_score_grad(const fltop_rows* logprobs, const fltop_hypotheses* hyp
  *     FLTOP_PREFERENCE_HINGE    max(0, 1 - beta h)
  *     FLTOP_PREFERENCE_SQUARE   (h - 1 / (2 beta))^2
  * The result is the mean over the pairs that take part: those before pair_counts[b] whose two
- * indices are in [0,N) and whose scores are all finite.  A pair may appear twice (it counts
+ * indices are in [0,N), whose scores are all finite and whose margin is.  A pair may appear twice (it counts
  * twice) and hypotheses may be shared by pairs (their gradients add up).  No pair: loss 0. */
 #define FLTOP_PREFERENCE_SIGMOID 0
 #define FLTOP_PREFERENCE_HINGE   1

@@ -95,7 +95,7 @@ extern "C" size_t fltop_preference_workspace_bytes(int32_t B) {
 extern "C" int fltop_preference_loss(const fltop_preference* p, void* workspace, size_t workspace_bytes,
                                      void* hip_stream) {
     if (!p || !p->scores || !p->pairs || !p->loss || !p->margins || !p->grad_scores) return FLTOP_ERR_NULL_POINTER;
-    if (p->B < 1 || p->N < 1 || p->M < 1 || (int64_t)p->M * 2 > (int64_t)INT32_MAX) return FLTOP_ERR_BAD_SHAPE;
+    if (p->B < 1 || p->N < 1 || p->M < 1 || p->M > (1 << 29)) return FLTOP_ERR_BAD_SHAPE;
     if (p->N > FLTOP_MAX_BEAM) return FLTOP_ERR_BAD_BEAM;
     const bool sigmoid = p->kind == FLTOP_PREFERENCE_SIGMOID;
     if (p->kind < FLTOP_PREFERENCE_SIGMOID || p->kind > FLTOP_PREFERENCE_SQUARE || !(p->beta > 0.0) ||

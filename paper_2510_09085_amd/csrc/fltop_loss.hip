@@ -2,9 +2,15 @@
 // better to the worse), and a clipped policy loss with a KL term.  Everything is fp64: the scores
 // are, and there are few of them.
 //
-// A mean over what takes part needs its number before the gradient: one workgroup per utterance
-// sums its own values, counts them and leaves the gradient unscaled; a second kernel adds the
-// utterances' sums up (each of its workgroups all of them, in one order) and scales.
+// A mean over what takes part needs its number before the gradient.  Small batches are one workgroup's, in one launch (64
+// pairs: 7.5 us, nearly all of it latency, where two launches took 10).
+// Else one workgroup per utterance sums its own values, counts them and leaves the gradient unscaled; a second kernel adds
+// the utterances' sums up (each of its workgroups all of them, in one order) and scales.
+//
+// A hypothesis may be in many pairs: its derivatives are added in LDS as whole multiples of 2^-50 of the utterances' largest one
+// (2^-S, S less, for lists of more than 2^11 pairs), so that the order in which threads add does not matter.  A pair's derivative
+// grows with its margin for each kind of loss, so the largest one is that of the smallest or of the largest margin: a first
+// pass over the pairs makes the margins, a second one the rest.
 #include "fltop_learn.h"
 
 namespace fltop {
@@ -12,6 +18,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWave = 64;
+constexpr int kOneThreads = 1024;    // of the one workgroup that takes a small batch
+constexpr int32_t kOneScores = 2048, kOnePairs = 4096, kOneEntries = 2048;
 
 // Sum over the workgroup in a fixed order; every thread gets it.
 __device__ double block_sum(double x, double* scratch) {
@@ -30,66 +38,135 @@ struct PairSums {
     double n;
 };
 
-// ln(1 + e^x)
-__device__ inline double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+__device__ inline double block_most(double x, double* scratch) {
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) x = fmax(x, __shfl_xor(x, o, kWave));
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) scratch[threadIdx.x / kWave] = x;
+    __syncthreads();
+    double s = scratch[0];
+    for (int w = 1; w < (int)blockDim.x / kWave; ++w) s = fmax(s, scratch[w]);
+    return s;
+}
 
-__global__ __launch_bounds__(kThreads) void preference_kernel(fltop_preference p, PairSums* sums) {
+// A pair's margin, loss and derivative; whether it takes part.
+__device__ inline bool pair_loss(const fltop_preference& p, double h, double* loss, double* slope) {
+    if (!isfinite(h)) return false;
+    const double x = p.beta * h;
+    if (p.kind == FLTOP_PREFERENCE_SIGMOID) {
+        const double e = exp(-fabs(x)), l = log1p(e);
+        // ln(1 + e^-x) and ln(1 + e^x), sigma(x)
+        *loss = (1.0 - p.label_smoothing) * (fmax(-x, 0.0) + l) + p.label_smoothing * (fmax(x, 0.0) + l);
+        // sigma(x) - (1 - label_smoothing), without cancellation where nothing is smoothed
+        *slope = p.beta * (p.label_smoothing - (x >= 0.0 ? e : 1.0) / (1.0 + e));
+    } else if (p.kind == FLTOP_PREFERENCE_HINGE) {
+        *loss = fmax(0.0, 1.0 - x);
+        *slope = x < 1.0 ? -p.beta : 0.0;
+    } else {
+        const double d = h - 0.5 / p.beta;
+        *loss = d * d;
+        *slope = fmin(fmax(2.0 * d, -1.7e308), 1.7e308);
+    }
+    return true;
+}
+
+__device__ inline double slope_of(const fltop_preference& p, double h) {
+    double f, g;
+    return pair_loss(p, h, &f, &g) ? fabs(g) : 0.0;
+}
+
+constexpr double kShift = 6755399441055744.0;   // 1.5 * 2^52: its last bit is worth one
+
+// How derivatives are kept as whole numbers: g as g * to, and back.
+struct Steps {
+    double to, back;
+    __device__ Steps(double most, int32_t M) {
+        const int bits = min(50, 61 - (32 - __clz(M)));
+        most = fmax(most, 1e-290);   // `to` stays finite
+        to = ldexp(1.0, bits) / most;
+        back = ldexp(most, -bits);
+    }
+    __device__ unsigned long long whole(double g) const {
+        return (unsigned long long)(__double_as_longlong(g * to + kShift) - __double_as_longlong(kShift));
+    }
+    __device__ double value(unsigned long long sum) const { return (double)(long long)sum * back; }
+};
+
+// Log ratio of a hypothesis to its reference, NaN if it takes no part.
+__device__ inline double log_ratio(const fltop_preference& p, int64_t at) {
+    const double s = p.scores[at], q = p.ref_scores ? p.ref_scores[at] : 0.0;
+    return isfinite(s) && isfinite(q) ? s - q : NAN;
+}
+
+__device__ inline int32_t pairs_of(const fltop_preference& p, int32_t b) {
+    const int32_t count = p.pair_counts ? p.pair_counts[b] : p.M;
+    return count < 0 ? 0 : (count > p.M ? p.M : count);
+}
+
+// One workgroup's utterances: all of them with ONE, else its own.  LDS holds their log ratios and their derivatives' sums.
+template <int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void preference_kernel(fltop_preference p, PairSums* sums) {
     extern __shared__ double shared[];
-    __shared__ double scratch[kThreads / kWave];
-    double* ratio = shared;           // [N] s - q
-    const int32_t b = blockIdx.x;
-    const double* s = p.scores + (int64_t)b * p.N;
-    const double* q = p.ref_scores ? p.ref_scores + (int64_t)b * p.N : nullptr;
-    for (int32_t n = threadIdx.x; n < p.N; n += kThreads) {
-        const bool fine = isfinite(s[n]) && (!q || isfinite(q[n]));
-        ratio[n] = fine ? (q ? s[n] - q[n] : s[n]) : NAN;
+    __shared__ double scratch[THREADS / kWave];
+    const int32_t b0 = ONE ? 0 : blockIdx.x, count = (ONE ? p.B : 1) * p.N;
+    const int64_t pairs = (int64_t)(ONE ? p.B : 1) * p.M;
+    double* const ratio = shared;
+    unsigned long long* const slopes = reinterpret_cast<unsigned long long*>(shared + count);
+    for (int32_t i = threadIdx.x; i < count; i += THREADS) {
+        ratio[i] = log_ratio(p, (int64_t)b0 * p.N + i);
+        slopes[i] = 0;
     }
     __syncthreads();
-    int32_t count = p.pair_counts ? p.pair_counts[b] : p.M;
-    count = count < 0 ? 0 : (count > p.M ? p.M : count);
-    const int32_t* pairs = p.pairs + (int64_t)b * p.M * 2;
-    double* margins = p.margins + (int64_t)b * p.M;
-    double loss = 0.0, used = 0.0;
-    for (int32_t m = threadIdx.x; m < p.M; m += kThreads) {
+    const int32_t* const list = p.pairs + (int64_t)b0 * p.M * 2;
+    double* const margins = p.margins + (int64_t)b0 * p.M;
+    auto pair_at = [&](int64_t m) {
+        int2 pair;
+        __builtin_memcpy(&pair, list + 2 * m, sizeof(pair));
+        return pair;
+    };
+    auto first_of = [&](int64_t m) { return ONE ? (int32_t)((uint32_t)m / (uint32_t)p.M) : 0; };
+    double high = -INFINITY, low = INFINITY;
+#pragma unroll 4
+    for (int64_t m = threadIdx.x; m < pairs; m += THREADS) {
+        const int32_t b = first_of(m);
+        const int2 pair = pair_at(m);
         double h = NAN;
-        if (m < count) {
-            const int32_t i = pairs[2 * m], j = pairs[2 * m + 1];
-            if ((uint32_t)i < (uint32_t)p.N && (uint32_t)j < (uint32_t)p.N) h = ratio[i] - ratio[j];
-        }
+        if ((int32_t)(m - (int64_t)b * p.M) < pairs_of(p, b0 + b) && (uint32_t)pair.x < (uint32_t)p.N &&
+            (uint32_t)pair.y < (uint32_t)p.N)
+            h = ratio[b * p.N + pair.x] - ratio[b * p.N + pair.y];
+        if (!isfinite(h)) h = NAN;
         margins[m] = h;
-        if (h != h) continue;
+        high = fmax(high, h);   // (NaN is passed over)
+        low = fmin(low, h);
+    }
+    high = block_most(high, scratch);
+    low = -block_most(-low, scratch);
+    const Steps steps(fmax(slope_of(p, high), slope_of(p, low)), p.M);
+    double loss = 0.0, used = 0.0;
+#pragma unroll 4
+    for (int64_t m = threadIdx.x; m < pairs; m += THREADS) {
+        const double h = margins[m];
+        const int2 pair = pair_at(m);
+        double f, g;
+        if (!pair_loss(p, h, &f, &g)) continue;
+        loss += f;
         used += 1.0;
-        const double x = p.beta * h;
-        if (p.kind == FLTOP_PREFERENCE_SIGMOID)
-            loss += (1.0 - p.label_smoothing) * softplus(-x) + p.label_smoothing * softplus(x);
-        else if (p.kind == FLTOP_PREFERENCE_HINGE)
-            loss += fmax(0.0, 1.0 - x);
-        else
-            loss += (h - 0.5 / p.beta) * (h - 0.5 / p.beta);
+        const unsigned long long whole = steps.whole(g);
+        const int32_t b = first_of(m);
+        atomicAdd(&slopes[b * p.N + pair.x], whole);
+        atomicAdd(&slopes[b * p.N + pair.y], 0ull - whole);
     }
     loss = block_sum(loss, scratch);
     used = block_sum(used, scratch);
-    if (threadIdx.x == 0) sums[b] = {loss, used};
-    // the margins are this workgroup's own writes: visible to it after the barriers in block_sum
-    for (int32_t n = threadIdx.x; n < p.N; n += kThreads) {
-        double d = 0.0;
-        for (int32_t m = 0; m < count; ++m) {
-            const int32_t i = pairs[2 * m], j = pairs[2 * m + 1];
-            if ((i != n && j != n) || i == j) continue;
-            const double h = margins[m];
-            if (h != h) continue;
-            const double x = p.beta * h;
-            double g;
-            if (p.kind == FLTOP_PREFERENCE_SIGMOID)
-                g = p.beta * (1.0 / (1.0 + exp(-x)) - (1.0 - p.label_smoothing));
-            else if (p.kind == FLTOP_PREFERENCE_HINGE)
-                g = x < 1.0 ? -p.beta : 0.0;
-            else
-                g = 2.0 * (h - 0.5 / p.beta);
-            d += i == n ? g : -g;
-        }
-        p.grad_scores[(int64_t)b * p.N + n] = d;
+    const double by = ONE ? (used > 0.0 ? p.scale / used : 0.0) : 1.0;
+    if (threadIdx.x == 0) {
+        if constexpr (ONE)
+            *p.loss = used > 0.0 ? loss / used : 0.0;
+        else
+            sums[b0] = {loss, used};
     }
+    for (int32_t i = threadIdx.x; i < count; i += THREADS)
+        p.grad_scores[(int64_t)b0 * p.N + i] = steps.value(slopes[i]) * by;
 }
 
 __global__ __launch_bounds__(kThreads) void preference_mean_kernel(fltop_preference p, const PairSums* sums) {
@@ -101,12 +178,29 @@ __global__ __launch_bounds__(kThreads) void preference_mean_kernel(fltop_prefere
     }
     loss = block_sum(loss, scratch);
     used = block_sum(used, scratch);
-    const double each = used > 0.0 ? 1.0 / used : 0.0;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.loss = loss * each;
+    const double by = used > 0.0 ? p.scale / used : 0.0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.loss = used > 0.0 ? loss / used : 0.0;
     const int64_t total = (int64_t)p.B * p.N;
     for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads)
-        p.grad_scores[i] *= each * p.scale;
+        p.grad_scores[i] *= by;
 }
+
+// An entry's numbers, and whether it takes part.
+struct Entry {
+    double l, old, ref, A;
+    bool part;
+    __device__ Entry(const double* scores, const double* old_scores, const double* ref_scores, const double* advantages,
+                     int64_t at, bool there) {
+        l = old = ref = A = 0.0;
+        if (there) {
+            l = scores[at];
+            old = old_scores[at];
+            A = advantages[at];
+            if (ref_scores) ref = ref_scores[at];
+        }
+        part = there && isfinite(l) && isfinite(old) && isfinite(A) && isfinite(ref);
+    }
+};
 
 __global__ __launch_bounds__(kThreads) void policy_kernel(const double* scores, const double* old_scores,
                                                           const double* ref_scores, const double* advantages,
@@ -119,14 +213,8 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(const double* scores, 
     PolicySums s = {0.0, 0.0, 0.0, 0.0};
     for (int32_t n = threadIdx.x; n < N; n += kThreads) {
         const int64_t at = (int64_t)b * N + n;
-        double d = 0.0;
-        if (n < count) {
-            const double l = scores[at], o = old_scores[at], A = advantages[at];
-            const double q = ref_scores ? ref_scores[at] : 0.0;
-            if (isfinite(l) && isfinite(o) && isfinite(A) && isfinite(q))
-                d = policy_entry(l, o, ref_scores != nullptr, q, A, p, &s);
-        }
-        grad_scores[at] = d;
+        const Entry e(scores, old_scores, ref_scores, advantages, at, n < count);
+        grad_scores[at] = e.part ? policy_entry(e.l, e.old, ref_scores != nullptr, e.ref, e.A, p, &s) : 0.0;
     }
     s.loss = block_sum(s.loss, scratch);
     s.kl = block_sum(s.kl, scratch);
@@ -188,6 +276,58 @@ __global__ __launch_bounds__(kThreads) void policy_mean_kernel(const PolicySums*
         grad_scores[i] *= policy_weight(sums[i / N].n, t, p.reduction) * p.scale;
 }
 
+// A small batch in one workgroup: rows' numbers in LDS, then the entries.
+__global__ __launch_bounds__(kOneThreads) void policy_one_kernel(const double* scores, const double* old_scores,
+                                                                 const double* ref_scores, const double* advantages,
+                                                                 const int32_t* counts, int32_t B, int32_t N,
+                                                                 fltop_policy p, double* summary, double* grad_scores) {
+    __shared__ int32_t numbers[kOneEntries];
+    __shared__ double scratch[kOneThreads / kWave];
+    constexpr int kEach = kOneEntries / kOneThreads;
+    const int32_t total = B * N;
+    for (int32_t b = threadIdx.x; b < B; b += kOneThreads) numbers[b] = 0;
+    __syncthreads();
+    double d[kEach];
+    int32_t row[kEach];
+    PolicySums mine[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int32_t at = k * kOneThreads + threadIdx.x, b = (uint32_t)at / (uint32_t)N;
+        row[k] = at < total ? b : -1;
+        const bool there = at < total && at - b * N < (counts ? counts[b] : N);
+        const Entry e(scores, old_scores, ref_scores, advantages, at, there);
+        mine[k] = {0.0, 0.0, 0.0, 0.0};
+        d[k] = e.part ? policy_entry(e.l, e.old, ref_scores != nullptr, e.ref, e.A, p, &mine[k]) : 0.0;
+        if (e.part) atomicAdd(&numbers[b], 1);
+    }
+    __syncthreads();
+    PolicyTotal t = {0.0, 0.0, 0.0, 0.0, 0.0};
+    for (int32_t b = threadIdx.x; b < B; b += kOneThreads) {
+        t.n += numbers[b];
+        t.rows += numbers[b] > 0 ? 1.0 : 0.0;
+    }
+    t.n = block_sum(t.n, scratch);
+    t.rows = block_sum(t.rows, scratch);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const double weight = row[k] >= 0 ? policy_weight(numbers[row[k]], t, p.reduction) : 0.0;
+        if (mine[k].n > 0.0) {
+            t.loss += mine[k].loss * weight;
+            t.kl += mine[k].kl * weight;
+            t.clipped += mine[k].clipped;
+        }
+        if (row[k] >= 0) grad_scores[k * kOneThreads + threadIdx.x] = mine[k].n > 0.0 ? d[k] * (weight * p.scale) : 0.0;
+    }
+    t.loss = block_sum(t.loss, scratch);
+    t.kl = block_sum(t.kl, scratch);
+    t.clipped = block_sum(t.clipped, scratch);
+    if (threadIdx.x == 0) {
+        summary[0] = t.loss;
+        summary[1] = t.kl;
+        summary[2] = t.n > 0.0 ? t.clipped / t.n : 0.0;
+    }
+}
+
 unsigned blocks_for(int64_t n) {
     const int64_t blocks = (n + kThreads - 1) / kThreads;
     return (unsigned)(blocks < 1024 ? blocks : 1024);
@@ -197,8 +337,20 @@ unsigned blocks_for(int64_t n) {
 
 hipError_t launch_preference(const fltop_preference& p, void* workspace, hipStream_t stream) {
     PairSums* sums = static_cast<PairSums*>(workspace);
-    hipLaunchKernelGGL(preference_kernel, dim3(p.B), dim3(kThreads), (size_t)p.N * sizeof(double), stream, p, sums);
-    hipLaunchKernelGGL(preference_mean_kernel, dim3(blocks_for((int64_t)p.B * p.N)), dim3(kThreads), 0, stream, p, sums);
+    const int64_t scores = (int64_t)p.B * p.N, pairs = (int64_t)p.B * p.M;
+    if (scores <= kOneScores && pairs <= kOnePairs) {
+        hipLaunchKernelGGL((preference_kernel<kOneThreads, true>), dim3(1), dim3(kOneThreads), (size_t)scores * 16, stream, p,
+                           sums);
+        return hipGetLastError();
+    }
+    // 128 utterances of 4950 pairs: 29 us with 256 threads, 20 us with 1024, about half of which are the exponentials and
+    // logarithms of the 128 compute units in use.
+    if (p.M > kThreads * 2)
+        hipLaunchKernelGGL((preference_kernel<kOneThreads, false>), dim3(p.B), dim3(kOneThreads), (size_t)p.N * 16, stream, p,
+                           sums);
+    else
+        hipLaunchKernelGGL((preference_kernel<kThreads, false>), dim3(p.B), dim3(kThreads), (size_t)p.N * 16, stream, p, sums);
+    hipLaunchKernelGGL(preference_mean_kernel, dim3(blocks_for(scores)), dim3(kThreads), 0, stream, p, sums);
     return hipGetLastError();
 }
 
@@ -207,6 +359,11 @@ hipError_t launch_policy(const double* scores, const double* old_scores, const d
                          const fltop_policy& policy, void* workspace, double* summary, double* grad_scores,
                          hipStream_t stream) {
     PolicySums* sums = static_cast<PolicySums*>(workspace);
+    if ((int64_t)B * N <= kOneEntries) {
+        hipLaunchKernelGGL(policy_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, scores, old_scores, ref_scores, advantages,
+                           counts, B, N, policy, summary, grad_scores);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(policy_kernel, dim3(B), dim3(kThreads), 0, stream, scores, old_scores, ref_scores, advantages,
                        counts, N, policy, sums, grad_scores);
     hipLaunchKernelGGL(policy_mean_kernel, dim3(blocks_for((int64_t)B * N)), dim3(kThreads), 0, stream, sums, B, N,
