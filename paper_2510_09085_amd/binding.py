@@ -7,6 +7,7 @@ missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -471,22 +472,24 @@ class _On:
     """The device of `t` made current, and outputs and workspaces taken on the stream that the call
     is enqueued on, so that they outlive their use there.  `stream` None: that device's current one."""
 
+    __slots__ = ("_managers", "_index", "_stream")
+
     def __init__(self, t: torch.Tensor, stream):
-        self._device = t.device if t.device.index != torch.cuda.current_device() else None
-        self._stream = stream
-        self._entered = []
+        self._index, self._stream, self._managers = t.device.index, stream, ()
+        if self._index != torch.cuda.current_device():
+            self._managers += (torch.cuda.device(t.device),)
+        if stream is not None:
+            self._managers += (torch.cuda.stream(stream),)
 
     def __enter__(self):
-        for manager in (self._device and torch.cuda.device(self._device),
-                        self._stream and torch.cuda.stream(self._stream)):
-            if manager is not None:
-                manager.__enter__()
-                self._entered.append(manager)
-        return _stream_handle(self._stream)
+        for manager in self._managers:
+            manager.__enter__()
+        stream = torch.cuda.current_stream(self._index) if self._stream is None else self._stream
+        return stream.cuda_stream
 
     def __exit__(self, *what):
-        while self._entered:
-            self._entered.pop().__exit__(*what)
+        for manager in reversed(self._managers):
+            manager.__exit__(*what)
 
 
 def _need(ok: bool, message: str):
@@ -496,21 +499,23 @@ def _need(ok: bool, message: str):
 
 def _device_tensor(t, name: str, dtype, shape, device):
     """Checks a dense tensor of one call (all of a call's tensors are on one device)."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return
     if not (t.is_cuda and t.device == device):
         raise ValueError(f"{name} must be on {device}, where the call's other tensors are")
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)}")
 
 
 def _rows(x: torch.Tensor, lengths: torch.Tensor, name: str) -> FltopRows:
     _need(x.is_cuda, f"{name} must be a device tensor")
-    _need(x.dtype in ROW_TYPES, f"{name} must be float32, bfloat16 or float16")
+    kind = ROW_TYPES.get(x.dtype)
+    _need(kind is not None, f"{name} must be float32, bfloat16 or float16")
     _need(x.dim() == 3 and x.numel() > 0, f"{name} must be a [B,T,V] tensor")
     B, T, V = x.shape
-    _need(x.stride(2) == 1 or V == 1, f"{name}: the V values of a row must be adjacent")
+    by_batch, by_frame, by_value = x.stride()
+    _need(by_value == 1 or V == 1, f"{name}: the V values of a row must be adjacent")
     _device_tensor(lengths, "lengths", torch.int32, (B,), x.device)
-    return FltopRows(x.data_ptr(), lengths.data_ptr(), x.stride(0), x.stride(1), B, T, V,
-                     ROW_TYPES[x.dtype])
+    return FltopRows(x.data_ptr(), lengths.data_ptr(), by_batch, by_frame, B, T, V, kind)
 
 
 def _hypotheses(tokens, token_lengths, counts, B: int, device) -> FltopHypotheses:
@@ -518,15 +523,20 @@ def _hypotheses(tokens, token_lengths, counts, B: int, device) -> FltopHypothese
           and tokens.dtype == torch.int32 and tokens.device == device,
           f"tokens must be an int32 [B,N,U] tensor on {device}")
     _, N, U = tokens.shape
-    _need(tokens.stride(2) == 1 or U == 1, "the tokens of a hypothesis must be adjacent")
-    _need(tuple(token_lengths.shape) == (B, N) and token_lengths.dtype == torch.int32
+    by_batch, by_hypothesis, by_token = tokens.stride()
+    _need(by_token == 1 or U == 1, "the tokens of a hypothesis must be adjacent")
+    _need(token_lengths.shape == (B, N) and token_lengths.dtype == torch.int32
           and token_lengths.device == device, f"token_lengths must be an int32 [B,N] tensor on {device}")
-    _need(token_lengths.stride(1) == 1 or N == 1, "the token lengths of an utterance must be adjacent")
+    lengths_by_batch, by_length = token_lengths.stride()
+    _need(by_length == 1 or N == 1, "the token lengths of an utterance must be adjacent")
     if counts is not None:
         _device_tensor(counts, "counts", torch.int32, (B,), device)
-    return FltopHypotheses(tokens.data_ptr(), token_lengths.data_ptr(),
-                           None if counts is None else counts.data_ptr(), tokens.stride(0),
-                           tokens.stride(1), token_lengths.stride(0), N, U)
+    return FltopHypotheses(tokens.data_ptr(), token_lengths.data_ptr(), _address(counts), by_batch,
+                           by_hypothesis, lengths_by_batch, N, U)
+
+
+def _address(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def _raise(rc: int, where: str):
@@ -534,11 +544,18 @@ def _raise(rc: int, where: str):
         raise FltopError(rc, where)
 
 
-def _workspace(workspace, nbytes: int, where: str, device) -> torch.Tensor:
-    if nbytes == 0:
+@functools.lru_cache(maxsize=256)
+def _bytes(where: str, *shape: int) -> int:
+    n = int(getattr(load(), where)(*shape))
+    if n == 0:
         raise FltopError(-2, where)
+    return n
+
+
+def _workspace(workspace, device, where: str, *shape: int) -> torch.Tensor:
+    """The caller's workspace, or one of the size that the library's function `where` gives."""
     if workspace is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return torch.empty(_bytes(where, *shape), dtype=torch.uint8, device=device)
     _need(workspace.device == device and workspace.is_contiguous() and workspace.dtype == torch.uint8,
           f"the workspace must be a contiguous uint8 tensor on {device}")
     return workspace
@@ -566,10 +583,9 @@ def ctc_score(logprobs: torch.Tensor, lengths: torch.Tensor, tokens: torch.Tenso
     with _On(logprobs, stream) as handle:
         out = {"scores": torch.empty((x.B, h.N), dtype=torch.float64, device=dev)}
         if want_grad or workspace is not None:
-            out["workspace"] = _workspace(workspace, score_workspace_bytes(x.B, x.T, h.N, h.U),
-                                          "fltop_ctc_score_workspace_bytes", dev)
+            out["workspace"] = _workspace(workspace, dev, "fltop_ctc_score_workspace_bytes", x.B, x.T, h.N, h.U)
         ws = out.get("workspace")
-        _raise(load().fltop_ctc_score(ctypes.byref(x), ctypes.byref(h), _ptr(out["scores"]), _ptr(ws),
+        _raise(load().fltop_ctc_score(ctypes.byref(x), ctypes.byref(h), _address(out["scores"]), _address(ws),
                                       0 if ws is None else ws.numel(), handle), "fltop_ctc_score")
     return out
 
@@ -585,11 +601,12 @@ def ctc_score_grad(logprobs: torch.Tensor, lengths: torch.Tensor, tokens: torch.
     dev = logprobs.device
     h = _hypotheses(tokens, token_lengths, counts, x.B, dev)
     _device_tensor(grad_scores, "grad_scores", torch.float64, (x.B, h.N), dev)
-    ws = _workspace(workspace, score_workspace_bytes(x.B, x.T, h.N, h.U), "fltop_ctc_score_workspace_bytes", dev)
+    _need(workspace is not None, "workspace must be the one that ctc_score returned")
+    ws = _workspace(workspace, dev, "fltop_ctc_score_workspace_bytes", x.B, x.T, h.N, h.U)
     with _On(logprobs, stream) as handle:
         grad = torch.empty((x.B, x.T, x.V), dtype=logprobs.dtype, device=dev)
-        _raise(load().fltop_ctc_score_grad(ctypes.byref(x), ctypes.byref(h), _ptr(grad_scores), _ptr(ws),
-                                           ws.numel(), _ptr(grad), handle), "fltop_ctc_score_grad")
+        _raise(load().fltop_ctc_score_grad(ctypes.byref(x), ctypes.byref(h), _address(grad_scores), _address(ws),
+                                           ws.numel(), _address(grad), handle), "fltop_ctc_score_grad")
     return grad
 
 
@@ -618,13 +635,12 @@ def preference_loss(scores: torch.Tensor, pairs: torch.Tensor, *,
         grad = torch.empty_like(scores)
         loss = torch.empty((), dtype=torch.float64, device=dev)
         margins = torch.empty((B, M), dtype=torch.float64, device=dev)
-        ws = _workspace(workspace, int(load().fltop_preference_workspace_bytes(B)),
-                        "fltop_preference_workspace_bytes", dev)
-        p = FltopPreference(scores.data_ptr(), None if ref_scores is None else ref_scores.data_ptr(),
-                            pairs.data_ptr(), None if pair_counts is None else pair_counts.data_ptr(),
+        ws = _workspace(workspace, dev, "fltop_preference_workspace_bytes", B)
+        p = FltopPreference(scores.data_ptr(), _address(ref_scores),
+                            pairs.data_ptr(), _address(pair_counts),
                             B, N, M, PREFERENCE_KINDS[kind], beta, label_smoothing, scale,
                             loss.data_ptr(), margins.data_ptr(), grad.data_ptr())
-        _raise(load().fltop_preference_loss(ctypes.byref(p), _ptr(ws), ws.numel(), handle),
+        _raise(load().fltop_preference_loss(ctypes.byref(p), _address(ws), ws.numel(), handle),
                "fltop_preference_loss")
     return {"loss": loss, "margins": margins, "grad_scores": grad}
 
@@ -655,11 +671,10 @@ def policy_loss(scores: torch.Tensor, old_scores: torch.Tensor, advantages: torc
     with _On(scores, stream) as handle:
         grad = torch.empty_like(scores)
         summary = torch.empty(3, dtype=torch.float64, device=dev)
-        ws = _workspace(workspace, int(load().fltop_policy_workspace_bytes(B, 1)),
-                        "fltop_policy_workspace_bytes", dev)
-        _raise(load().fltop_policy_loss(_ptr(scores), _ptr(old_scores), _ptr(ref_scores), _ptr(advantages),
-                                        _ptr(counts), B, N, ctypes.byref(p), _ptr(ws), ws.numel(),
-                                        _ptr(summary), _ptr(grad), handle), "fltop_policy_loss")
+        ws = _workspace(workspace, dev, "fltop_policy_workspace_bytes", B, 1)
+        _raise(load().fltop_policy_loss(_address(scores), _address(old_scores), _address(ref_scores), _address(advantages),
+                                        _address(counts), B, N, ctypes.byref(p), _address(ws), ws.numel(),
+                                        _address(summary), _address(grad), handle), "fltop_policy_loss")
     loss, kl, clipped = summary.unbind()
     return {"loss": loss, "kl": kl, "clipped": clipped, "grad_scores": grad}
 
@@ -689,12 +704,11 @@ def policy_loss_logits(logits: torch.Tensor, tokens: torch.Tensor, lengths: torc
         grad = torch.empty((x.B, x.T, x.V), dtype=logits.dtype, device=dev)
         logps = torch.empty(shape, dtype=torch.float32, device=dev)
         summary = torch.empty(3, dtype=torch.float32, device=dev)
-        ws = _workspace(workspace, int(load().fltop_policy_workspace_bytes(x.B, x.T)),
-                        "fltop_policy_workspace_bytes", dev)
-        _raise(load().fltop_policy_loss_logits(ctypes.byref(x), _ptr(tokens), _ptr(old_logps),
-                                               _ptr(ref_logps), _ptr(advantages), int(per_frame),
-                                               ctypes.byref(p), _ptr(ws), ws.numel(), _ptr(summary),
-                                               _ptr(logps), _ptr(grad), handle),
+        ws = _workspace(workspace, dev, "fltop_policy_workspace_bytes", x.B, x.T)
+        _raise(load().fltop_policy_loss_logits(ctypes.byref(x), _address(tokens), _address(old_logps),
+                                               _address(ref_logps), _address(advantages), int(per_frame),
+                                               ctypes.byref(p), _address(ws), ws.numel(), _address(summary),
+                                               _address(logps), _address(grad), handle),
                "fltop_policy_loss_logits")
     loss, kl, clipped = summary.unbind()
     return {"loss": loss, "kl": kl, "clipped": clipped, "logps": logps, "grad_logits": grad}
