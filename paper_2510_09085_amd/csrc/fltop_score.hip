@@ -177,35 +177,35 @@ struct alignas(8) Edge {
     int32_t aligned;
 };
 
-// A workgroup's LDS: edges of each direction and wavefront (one below the first) for this turn and the one before;
-// a place for what is written so that the lanes that have nothing to say need no branch; tables of exponentials of
+// A workgroup's LDS: edges of each of its directions (`side`) and wavefronts (one below the first) for this turn and the one
+// before; a place for what is written so that the lanes that have nothing to say need no branch; tables of exponentials of
 // W + 1 blocks, and whether one of them is out of range.  In the middle, masses of U + 1 states in place of the last two.
-template <int R, bool TABLE>
+template <int R, bool TABLE, int SIDES>
 struct Lds {
-    Edge<R>* edges;      // [2][W + 1][2]
-    int32_t* wide;       // [2][W + 1]
-    double* nowhere;     // [2 W][kWave + R]
-    double* tables;      // [2][W + 1][R][kTabulated]
+    Edge<R>* edges;      // [SIDES][W + 1][2]
+    int32_t* wide;       // [SIDES][W + 1]
+    double* nowhere;     // [SIDES W][kWave + R]
+    double* tables;      // [SIDES][W + 1][R][kTabulated]
     double* half_m;      // [U + 1]
     int32_t* half_e;
     int W;
 
     __device__ Lds(char* at, int waves, int32_t U) : W(waves) {
         edges = reinterpret_cast<Edge<R>*>(at);
-        wide = reinterpret_cast<int32_t*>(edges + 4 * (W + 1));
+        wide = reinterpret_cast<int32_t*>(edges + 2 * SIDES * (W + 1));
         nowhere = half_m = reinterpret_cast<double*>(wide + 2 * (W + 1));
-        tables = nowhere + 2 * W * (kWave + R);
+        tables = nowhere + SIDES * W * (kWave + R);
         half_e = reinterpret_cast<int32_t*>(half_m + U + 1);
     }
-    static size_t bytes(int W, int32_t U, bool middle) {
-        const size_t tables = TABLE ? 2 * (W + 1) * R * kTabulated : 0;
-        const size_t way = (2 * W * (kWave + R) + tables) * sizeof(double), half = middle ? (size_t)(U + 1) * 12 : 0;
-        return 4 * (W + 1) * sizeof(Edge<R>) + 2 * (W + 1) * sizeof(int32_t) + (way > half ? way : half);
+    static size_t bytes(int W, int32_t U) {
+        const size_t tables = TABLE ? SIDES * (W + 1) * R * kTabulated : 0;
+        const size_t way = (SIDES * W * (kWave + R) + tables) * sizeof(double), half = SIDES == 2 ? (size_t)(U + 1) * 12 : 0;
+        return 2 * SIDES * (W + 1) * sizeof(Edge<R>) + 2 * (W + 1) * sizeof(int32_t) + (way > half ? way : half);
     }
-    __device__ Edge<R>& edge(bool reversed, int wave_below, int turn) const {
-        return edges[((reversed ? W + 1 : 0) + wave_below) * 2 + (turn & 1)];
+    __device__ Edge<R>& edge(int side, int wave_below, int turn) const {
+        return edges[(side * (W + 1) + wave_below) * 2 + (turn & 1)];
     }
-    __device__ int slot(bool reversed, int32_t block) const { return (reversed ? W + 1 : 0) + block % (W + 1); }
+    __device__ int slot(int side, int32_t block) const { return side * (W + 1) + block % (W + 1); }
     __device__ double* table(int slot) const { return tables + slot * (R * kTabulated); }
 };
 
@@ -213,6 +213,7 @@ struct Lds {
 struct Way {
     int32_t lo, hi;      // its frames
     bool reversed;
+    int side;            // its part of the LDS
     Mark* marks;         // masses at the borders of blocks, [blocks][row] (or NULL), pair by pair as the direction sees them
     int32_t row;
 };
@@ -565,13 +566,13 @@ struct Tabulator {
     }
 };
 
-template <int R>
+template <int R, int SIDES>
 __device__ inline void tabulate_all(const Way& way, const Way& other, const Source& from, int32_t used,
-                                    const Lds<R, true>& lds) {
+                                    const Lds<R, true, SIDES>& lds) {
     const Blocks<R> blocks(way, other, used);
     Tabulator<R> even, odd;
     auto put = [&](Tabulator<R>& one, int32_t n) {
-        const int slot = lds.slot(way.reversed, n);
+        const int slot = lds.slot(way.side, n);
         one.put(from, lds.table(slot), lds.wide + slot);
     };
     if (blocks.count > 0) {
@@ -597,13 +598,13 @@ __device__ inline void tabulate_all(const Way& way, const Way& other, const Sour
 }
 
 // A wavefront's blocks.
-template <int K, int R, bool TABLE>
+template <int K, int R, bool TABLE, int SIDES>
 __device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way& other, int32_t L, const Source& from,
-                                int wave, int32_t used, const Lds<R, TABLE>& lds) {
-    double* const nowhere = lds.nowhere + ((way.reversed ? lds.W : 0) + wave) * (kWave + R);
+                                int wave, int32_t used, const Lds<R, TABLE, SIDES>& lds) {
+    double* const nowhere = lds.nowhere + (way.side * lds.W + wave) * (kWave + R);
     if (wave == 0 && threadIdx.x % kWave < 2 * R) {   // nothing comes from below the first
         const int32_t f = threadIdx.x & (R - 1);
-        Edge<R>& none = lds.edge(way.reversed, 0, threadIdx.x % kWave / R);
+        Edge<R>& none = lds.edge(way.side, 0, threadIdx.x % kWave / R);
         none.x[f] = 0.0;
         none.e[f] = kNoMass;
         none.E = kNoMass;
@@ -625,15 +626,15 @@ __device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way&
         const int32_t n = turn - wave;
         bool wide = true;
         if constexpr (TABLE) {
-            const int slot = lds.slot(way.reversed, n);
+            const int slot = lds.slot(way.side, n);
             wide = __builtin_amdgcn_readfirstlane(lds.wide[slot]);
             z.look_up(lds.table(slot));
         } else {
             z.got(from.type);
             ask(n + 1);
         }
-        take_block<K, R, TABLE>(z, way, L, blocks[n], wide, lds.edge(way.reversed, wave, turn - 1),
-                                lds.edge(way.reversed, wave + 1, turn), nowhere, from);
+        take_block<K, R, TABLE>(z, way, L, blocks[n], wide, lds.edge(way.side, wave, turn - 1),
+                                lds.edge(way.side, wave + 1, turn), nowhere, from);
         __syncthreads();
     }
     for (int32_t turn = after; turn < blocks.turns; ++turn) __syncthreads();
@@ -652,60 +653,62 @@ __host__ __device__ inline int32_t middle_of(int32_t frames) {
     return h < frames ? h : frames;
 }
 
-// A wavefront's part in its workgroup: W wavefronts of one direction, then one that tabulates for it, then the other's.
-template <int K, bool TABLE>
+// A wavefront's part in its workgroup: of each of its directions W wavefronts, then one that tabulates for them.
+template <int K, bool TABLE, int SIDES>
 struct Role {
-    int W, wave, lane;
-    bool reversed, tabulates;
+    int W, wave, side, lane;
+    bool tabulates;
     __device__ Role() {
-        const int n = (int)blockDim.x / kWave / 2;   // of a direction
+        const int n = (int)blockDim.x / kWave / SIDES;   // of a direction
         const int all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
         W = TABLE ? n - 1 : n;
-        reversed = all >= n;
-        wave = all - (reversed ? n : 0);
+        side = SIDES == 2 && all >= n ? 1 : 0;
+        wave = all - side * n;
         tabulates = TABLE && wave == W;
         lane = threadIdx.x & (kWave - 1);
     }
     __device__ int32_t first_pair() const { return (wave * kWave + lane) * K; }
 };
 
-// Scores; with KEEP also the masses at the borders of blocks, of both directions.
-template <int K, int R, int THREADS, bool TABLE, bool KEEP>
-__global__ __launch_bounds__(THREADS) void score_kernel(fltop_rows x, fltop_hypotheses h, double* out_scores,
-                                                        ScoreSpace ws) {
+// Scores, both directions of a hypothesis in a workgroup.  With KEEP each in one of its own: scores by the forward one, and
+// the masses at the borders of blocks by both.
+template <int K, int R, int WAVES, int THREADS, bool TABLE, bool KEEP>
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void score_kernel(
+    fltop_rows x, fltop_hypotheses h, double* out_scores, ScoreSpace ws) {
+    constexpr int kSides = KEEP ? 1 : 2;
     extern __shared__ char dynamic[];
     __shared__ Mass sums[kMostWaves];
     __shared__ Mass last[kMostWaves];
-    const int64_t at = blockIdx.x;
+    const int64_t at = KEEP ? blockIdx.x / 2 : blockIdx.x;
     const int32_t b = (int32_t)(at / h.N), n = (int32_t)(at % h.N);
     const Hyp y = hypothesis(x, h, b, n);
-    const Role<K, TABLE> role;
-    const Lds<R, TABLE> lds(dynamic, role.W, h.U);
-    const bool reversed = role.reversed;
+    const Role<K, TABLE, kSides> role;
+    const Lds<R, TABLE, kSides> lds(dynamic, role.W, h.U);
+    const bool reversed = KEEP ? blockIdx.x % 2 : role.side;
     Lane<K, R, TABLE> z;
     // (the lanes of a wavefront that tabulates lie behind the last pair)
     const bool fine = y.L >= 0 && z.start(y, x.V, reversed, role.tabulates ? y.L + 1 : role.first_pair());
     if (__syncthreads_or(!fine)) {
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && !(KEEP && reversed)) {
             out_scores[at] = y.L == -2 ? NAN : -INFINITY;
             if (KEEP) ws.total_m[at] = 0.0, ws.total_e[at] = kNoMass;
         }
         return;
     }
     const int32_t used = y.L / (kWave * K) + 1;
-    const int32_t middle = KEEP ? y.frames : middle_of<R>(y.frames);
-    Mark* const marks = KEEP ? ws.marks + at * 2 * ws.marks_of : nullptr;
-    const Way forward = {0, middle, false, marks, (int32_t)ws.row};
-    const Way backward = {KEEP ? 0 : middle, y.frames, true, KEEP ? marks + ws.marks_of : nullptr, (int32_t)ws.row};
-    const Way way = reversed ? backward : forward, other = reversed ? forward : backward;
+    const int32_t middle = middle_of<R>(y.frames);
+    const Way way = {!KEEP && reversed ? middle : 0, KEEP || reversed ? y.frames : middle, reversed, role.side,
+                     KEEP ? ws.marks + (at * 2 + reversed) * ws.marks_of : nullptr, (int32_t)ws.row};
+    const Way other = KEEP ? way : Way{reversed ? 0 : middle, reversed ? middle : y.frames, !reversed, 1 - role.side, nullptr, 0};
     if (role.tabulates) {
-        if constexpr (TABLE) tabulate_all<R>(way, other, source_of(x, b), used, lds);
+        if constexpr (TABLE) tabulate_all<R, kSides>(way, other, source_of(x, b), used, lds);
     } else {
-        take_all<K, R, TABLE>(z, way, other, y.L, source_of(x, b), role.wave, used, lds);
+        take_all<K, R, TABLE, kSides>(z, way, other, y.L, source_of(x, b), role.wave, used, lds);
     }
     if constexpr (KEEP) {
         // P = b_L + l_{L-1} after the last frame
-        if (!reversed && !role.tabulates) {
+        if (reversed) return;
+        if (!role.tabulates) {
             Mass end = no_mass();
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -1118,20 +1121,20 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
 }
 
 // Pairs of a lane, frames of a block, most threads.
-template <int K, int R, int THREADS, bool TABLE>
+template <int K, int R, int WAVES, bool TABLE>
 struct Build {
-    static unsigned threads(int W) { return 2 * kWave * (TABLE ? W + 1 : W); }
+    // (as many wavefronts as U can need: of 2 pairs 7 or 4, of 4 pairs 4, of 8 pairs 8; and the one that tabulates)
+    static constexpr int kMost = (K == 2 && WAVES == 4 ? 7 : K < 8 ? 4 : 8) + (TABLE ? 1 : 0);
     static hipError_t score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
                             hipStream_t stream) {
-        const int W = waves_for(h.U, K);
-        const dim3 grid((unsigned)(x.B * h.N)), block(threads(W));
-        const size_t bytes = Lds<R, TABLE>::bytes(W, h.U, true);
+        const int W = waves_for(h.U, K), threads = kWave * (TABLE ? W + 1 : W);
+        const unsigned hyps = (unsigned)(x.B * h.N);
         if (keep)
-            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, true>), grid, block, bytes, stream, x, h, out_scores,
-                               *keep);
+            hipLaunchKernelGGL((score_kernel<K, R, WAVES, kWave * kMost, TABLE, true>), dim3(2 * hyps), dim3(threads),
+                               (Lds<R, TABLE, 1>::bytes(W, h.U)), stream, x, h, out_scores, *keep);
         else
-            hipLaunchKernelGGL((score_kernel<K, R, THREADS, TABLE, false>), grid, block, bytes, stream, x, h, out_scores,
-                               ScoreSpace{});
+            hipLaunchKernelGGL((score_kernel<K, R, WAVES, 2 * kWave * kMost, TABLE, false>), dim3(hyps), dim3(2 * threads),
+                               (Lds<R, TABLE, 2>::bytes(W, h.U)), stream, x, h, out_scores, ScoreSpace{});
         return hipGetLastError();
     }
 };
@@ -1146,10 +1149,10 @@ hipError_t with_build(const fltop_rows& x, const fltop_hypotheses& h, F f) {
             // not fill the chip twice (64 transcripts of 229 tokens: 104 us, 128 with the other build); else for four, of up to
             // seven a direction (2048 hypotheses of 229: 300 us, 384 with the first).
             if (h.U < 512 && (int64_t)x.B * h.N < 512)
-                return table ? f(Build<2, 8, 640, true>{}) : f(Build<2, 8, 512, false>{});
-            return table ? f(Build<2, 8, 1024, true>{}) : f(Build<2, 8, 1024, false>{});
-        case 4: return table ? f(Build<4, 4, 640, true>{}) : f(Build<4, 4, 512, false>{});
-        default: return f(Build<8, 4, 1024, false>{});
+                return table ? f(Build<2, 8, 3, true>{}) : f(Build<2, 8, 3, false>{});
+            return table ? f(Build<2, 8, 4, true>{}) : f(Build<2, 8, 4, false>{});
+        case 4: return table ? f(Build<4, 4, 3, true>{}) : f(Build<4, 4, 3, false>{});
+        default: return f(Build<8, 4, 4, false>{});
     }
 }
 
