@@ -51,13 +51,14 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 // Every mass has its own exponent (class Mass), but aligning three of them for each sum costs more
 // than the sum.  So a block is entered with one exponent E for each lane, no smaller than that of any
 // mass that can reach the lane within the block (those of the kReach lanes below), and if
-//   - no mass of these lanes is below 2^(E - kSpread),
-//   - no emission needed in the block is below 2^-58 (e^-40) or from 2^14 up, and
-//   - the block has all its R frames
+//   - no mass of these lanes is below 2^(E - kSpread), and
+//   - no emission needed in the block is below 2^-58 (e^-40) or from 2^14 up,
 // then nothing leaves the range of fp64: masses stay above 2^(E - kSpread - 58 R) and below 2^(E + 128)
-// until its end.  A frame is then three multiply-adds and two products for each pair.  Blocks that do
-// not hold this (masks of -inf, masses of e^-3000 that may be needed yet) are gone through with
-// aligned exponents.  Rows of a trained model stay within: 10 tokens at e^-25 are 360 bits.
+// until its end.  Of the lanes below a lane whose states all have mass only that lane's own count: what
+// reaches it and leaves fp64 is below 2^-1022 of E, where each sum has a term of its own of 2^-957 at least
+// (K = 2), so that nothing of 64 bits is lost.  A frame is then three multiply-adds and two products for each
+// pair.  Blocks that do not hold this (masks of -inf, masses of e^-3000 that may be needed yet) are gone
+// through with aligned exponents.  Rows of a trained model stay within: 10 tokens at e^-25 are 360 bits.
 //
 // The exponential of an emission takes three times the frame's own work.  For vocabularies of up to
 // kTabulated tokens a wavefront more for each direction takes all of a block's, a turn ahead, into a
@@ -83,10 +84,10 @@ __device__ inline double from_lane(double x, int lane) {
                       __builtin_amdgcn_readlane((int32_t)a, lane));
 }
 
-// 2^e for e in [-1022, 1023].
+// 2^e for e in [-1022, 1023], and 0 for -1023.
 __device__ inline double power_of_two(int32_t e) { return from_words((e + 1023) << 20, 0); }
 // 2^e as a factor of masses of which those that leave the range are 0.
-__device__ inline double rescaling(int32_t e) { return power_of_two(max(min(e, 1000), -1022)); }
+__device__ inline double rescaling(int32_t e) { return power_of_two(max(min(e, 1000), -1023)); }
 __device__ inline uint32_t high_word(double x) { return (uint32_t)(__double_as_longlong(x) >> 32); }
 
 // Emissions that a block may have to be gone through with one exponent for each lane.
@@ -145,9 +146,6 @@ __device__ inline float raw_value(uint32_t x, int32_t type) {
 __device__ inline float value_at(const char* row, int32_t v, int32_t type) {
     return raw_value(type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, v) : raw_at<FLTOP_TYPE_F16>(row, v), type);
 }
-
-template <bool FIRST, typename A, typename B> struct Choose { using type = A; };
-template <typename A, typename B> struct Choose<false, A, B> { using type = B; };
 
 // An utterance's emissions.
 struct Source {
@@ -222,7 +220,7 @@ struct Way {
 template <int K, int R, bool TABLE>
 struct Lane {
     static constexpr int kReach = (R + K - 1) / K;   // lanes that a block's masses can come from
-    static constexpr int kSpread = 1017 - 58 * R;
+    static constexpr int kSpread = 957 - 58 * R;
 
     double xb[K], xl[K];     // masses x * 2^E, or x * 2^eb and x * 2^el if not `common`
     int32_t E, eb[K], el[K];
@@ -232,10 +230,9 @@ struct Lane {
     double live[K];          // 1 for pairs with a token, else 0
     int32_t i0;              // first pair
     // Without a table: emissions of the next block as they lie in memory, those of the present one, the blank's of frame f
-    // in lane f (mod R).  With one: the exponentials of the present block.
+    // in lane f (mod R).
     uint32_t raw[TABLE ? 1 : R][K], raw_blank;
-    using Given = typename Choose<TABLE, double, float>::type;
-    Given given[R][K], given_blank[TABLE ? R : 1];
+    float given[TABLE ? 1 : R][K], given_blank;
 
     __device__ bool start(const Hyp& y, int32_t V, bool reversed, int32_t first_pair) {
         bool fine = true;
@@ -284,8 +281,8 @@ struct Lane {
 #pragma unroll
         for (int f = 0; f < R; ++f)
 #pragma unroll
-            for (int k = 0; k < K; ++k) given[f][k] = raw_as<TYPE>(raw[TABLE ? 0 : f][k]);
-        given_blank[0] = raw_as<TYPE>(raw_blank);
+            for (int k = 0; k < K; ++k) given[TABLE ? 0 : f][k] = raw_as<TYPE>(raw[TABLE ? 0 : f][k]);
+        given_blank = raw_as<TYPE>(raw_blank);
     }
     __device__ void got(int32_t type) {
         if (type == FLTOP_TYPE_F32)
@@ -295,30 +292,22 @@ struct Lane {
         else
             got_as<FLTOP_TYPE_F16>();
     }
-    __device__ void look_up(const double* table) {
-#pragma unroll
-        for (int f = 0; f < R; ++f) {
-            given_blank[TABLE ? f : 0] = table[f * kTabulated];
-#pragma unroll
-            for (int k = 0; k < K; ++k) given[f][k] = table[f * kTabulated + tok[k]];
-        }
-    }
 
     // Whether this lane's emissions of the block are in range.
-    __device__ bool in_range() const {
+    __device__ bool in_range(const double* table) const {
         if constexpr (TABLE) {
             uint32_t most = 0, least = kMostWord;
-#pragma unroll
+#pragma unroll 1
             for (int f = 0; f < R; ++f)
 #pragma unroll
                 for (int k = -1; k < K; ++k) {
-                    const uint32_t w = high_word(k < 0 ? given_blank[f] : given[f][k < 0 ? 0 : k]);
+                    const uint32_t w = high_word(table[f * kTabulated + (k < 0 ? 0 : tok[k < 0 ? 0 : k])]);
                     most = max(most, w);
                     least = min(least, w);
                 }
             return least >= kLeastWord && most < kMostWord;
         } else {
-            float most = given_blank[0], least = given_blank[0];
+            float most = given_blank, least = given_blank;
 #pragma unroll
             for (int f = 0; f < R; ++f)
 #pragma unroll
@@ -334,6 +323,9 @@ struct Lane {
     // is within bounds.
     __device__ bool enter(const Edge<R>& in, int32_t* to, int32_t* least, int32_t* below) const {
         int32_t top = kNoMass, low = -kNoMass;
+        bool full = true;
+#pragma unroll
+        for (int k = 0; k < K; ++k) full &= xb[k] != 0.0 && (xl[k] != 0.0 || live[k] == 0.0);
         if (common) {
             uint32_t most = 0, few = UINT32_MAX;   // high words; less one, so that 0 is none
 #pragma unroll
@@ -356,10 +348,11 @@ struct Lane {
             }
         }
         int32_t m = top, n = low;
+        const int32_t others = full ? -kNoMass : -2147483647 - 1;   // those of the lanes below count from here up
 #pragma unroll
         for (int d = 0; d < kReach; ++d) {
             m = max(from_below(m, in.E), top);
-            n = min(from_below(n, in.least), low);
+            n = min(max(from_below(n, in.least), others), low);
         }
         *to = m;
         *least = n;
@@ -412,13 +405,24 @@ __device__ inline double sums_by_lane(double (&v)[R]) {
     return v[0];
 }
 
-// One block of frames for one wavefront.  `in`: from the wavefront below, `out`: for the one above.
-template <int K, int R, bool TABLE>
-__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t L, int32_t q, bool wide, const Edge<R>& in,
+// One block of frames for one wavefront.  `in`: from the wavefront below, `out`: for the one above.  AHEAD: a table's
+// exponentials are read before all else, into registers.
+template <int K, int R, bool TABLE, bool AHEAD>
+__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t q, const double* table, bool wide, const Edge<R>& in,
                                   Edge<R>& out, double* nowhere, const Source& from) {
     const int lane = threadIdx.x & (kWave - 1);
     const int32_t t0 = q * R;
     const int32_t nf = min(R, way.hi - t0);
+    constexpr bool kRead = TABLE && AHEAD;
+    double blanks[kRead ? R : 1], tokens[kRead ? R : 1][K];
+    if constexpr (kRead) {
+#pragma unroll
+        for (int f = 0; f < R; ++f) {
+            blanks[f] = table[f * kTabulated];
+#pragma unroll
+            for (int k = 0; k < K; ++k) tokens[f][k] = table[f * kTabulated + z.tok[k]];
+        }
+    }
     if (way.marks) {
         // (every lane has its place, with or without mass)
         Mark* const to = way.marks + (int64_t)q * way.row + z.i0;
@@ -427,8 +431,8 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
             to[k] = {z.xb[k], z.xl[k], z.common ? z.E : z.eb[k], z.common ? z.E : z.el[k]};
     }
     int32_t E, least, below;
-    bool fine = z.enter(in, &E, &least, &below) && nf == R && !in.aligned;
-    if (!TABLE || wide) fine &= z.in_range();
+    bool fine = z.enter(in, &E, &least, &below) && !in.aligned;
+    if (!TABLE || wide) fine &= z.in_range(table);
     const bool near = __all(fine);
     if (lane == kWave - 1) {
         out.E = E;
@@ -440,21 +444,10 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
         const double fx = rescaling(below - E);
         const double fskip = fx * z.skip[0];
         double* const edge = lane == kWave - 1 ? out.x : nowhere + lane;
-        double first[R];
-#pragma unroll
-        for (int f = 0; f < R; ++f) first[f] = in.x[f];
         z.rescale(E);
-        double blank_by_lane = 0.0;
-        if constexpr (!TABLE) blank_by_lane = exp_near(z.given_blank[0]);
-#pragma unroll
-        for (int f = 0; f < R; ++f) {
-            double pb;
-            if constexpr (TABLE)
-                pb = z.given_blank[f];
-            else
-                pb = from_lane(blank_by_lane, f);
-            edge[f] = z.xl[K - 1];
-            const double moved = from_below(z.xl[K - 1], first[f]);
+        auto take_frame = [&](double* edge_at, double first, double pb, auto token_p) {
+            *edge_at = z.xl[K - 1];
+            const double moved = from_below(z.xl[K - 1], first);
 #pragma unroll
             for (int k = K - 1; k >= 0; --k) {
                 const double prev = k > 0 ? z.xl[k > 0 ? k - 1 : 0] : moved;
@@ -462,10 +455,30 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
                 const double l = fma(prev, k > 0 ? z.skip[k] : fskip, stay);
                 const double b = k > 0 ? z.xb[k] + prev : fma(prev, fx, z.xb[k]);
                 z.xb[k] = b * pb;
-                if constexpr (TABLE)
-                    z.xl[k] = l * z.given[f][k];
-                else
-                    z.xl[k] = l * exp_near(z.given[f][k]);
+                z.xl[k] = l * token_p(k);
+            }
+        };
+        if (nf == R) {
+            double first[R];
+#pragma unroll
+            for (int f = 0; f < R; ++f) first[f] = in.x[f];
+            double blank_by_lane = 0.0;
+            if constexpr (!TABLE) blank_by_lane = exp_near(z.given_blank);
+#pragma unroll
+            for (int f = 0; f < R; ++f) {
+                const double pb = kRead ? blanks[kRead ? f : 0] : TABLE ? table[f * kTabulated] : from_lane(blank_by_lane, f);
+                take_frame(edge + f, first[f], pb, [&](int k) {
+                    return kRead   ? tokens[kRead ? f : 0][k]
+                           : TABLE ? table[f * kTabulated + z.tok[k]]
+                                   : exp_near(z.given[TABLE ? 0 : f][k]);
+                });
+            }
+        } else {   // an utterance's last block, its emissions from memory once more
+#pragma unroll 1
+            for (int f = 0; f < nf; ++f) {
+                const char* row = from.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - f : f)) * from.frame_bytes;
+                take_frame(edge + f, in.x[f], exp_near(value_at(row, 0, from.type)),
+                           [&](int k) { return exp_near(value_at(row, z.tok[k], from.type)); });
             }
         }
     } else {
@@ -598,9 +611,9 @@ __device__ inline void tabulate_all(const Way& way, const Way& other, const Sour
 }
 
 // A wavefront's blocks.
-template <int K, int R, bool TABLE, int SIDES>
-__device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way& other, int32_t L, const Source& from,
-                                int wave, int32_t used, const Lds<R, TABLE, SIDES>& lds) {
+template <int K, int R, bool TABLE, bool AHEAD, int SIDES>
+__device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way& other, const Source& from, int wave,
+                                int32_t used, const Lds<R, TABLE, SIDES>& lds) {
     double* const nowhere = lds.nowhere + (way.side * lds.W + wave) * (kWave + R);
     if (wave == 0 && threadIdx.x % kWave < 2 * R) {   // nothing comes from below the first
         const int32_t f = threadIdx.x & (R - 1);
@@ -625,15 +638,16 @@ __device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way&
     for (int32_t turn = before; turn < after; ++turn) {
         const int32_t n = turn - wave;
         bool wide = true;
+        const double* table = nullptr;
         if constexpr (TABLE) {
             const int slot = lds.slot(way.side, n);
             wide = __builtin_amdgcn_readfirstlane(lds.wide[slot]);
-            z.look_up(lds.table(slot));
+            table = lds.table(slot);
         } else {
             z.got(from.type);
             ask(n + 1);
         }
-        take_block<K, R, TABLE>(z, way, L, blocks[n], wide, lds.edge(way.side, wave, turn - 1),
+        take_block<K, R, TABLE, AHEAD>(z, way, blocks[n], table, wide, lds.edge(way.side, wave, turn - 1),
                                 lds.edge(way.side, wave + 1, turn), nowhere, from);
         __syncthreads();
     }
@@ -703,7 +717,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
     if (role.tabulates) {
         if constexpr (TABLE) tabulate_all<R, kSides>(way, other, source_of(x, b), used, lds);
     } else {
-        take_all<K, R, TABLE, kSides>(z, way, other, y.L, source_of(x, b), role.wave, used, lds);
+        take_all<K, R, TABLE, K == 2 && WAVES == 3, kSides>(z, way, other, source_of(x, b), role.wave, used, lds);
     }
     if constexpr (KEEP) {
         // P = b_L + l_{L-1} after the last frame
@@ -814,9 +828,10 @@ __device__ inline double from_above(double x) {
 }
 
 // 2^c by which the product of two masses of exponents that add up to c becomes an occupancy, less that of P.  Masses are
-// below 2^128, so that an occupancy of weight has c > -300; up to kMostShift one mass times 2^c stays in range whatever
-// the other is.
-constexpr int32_t kMostShift = 880;
+// below 2^128 in these exponents, so that an occupancy of weight (2^-50 up) has c > -306, and with c up to kMostShift
+// both its masses are above 2^-678: what leaves the range of fp64 has none, nor has what passes an emission below e^-600,
+// for which exp_any gives that.
+constexpr int32_t kMostShift = 500;
 __device__ inline int32_t share_shift(int32_t Ef, int32_t Eb, int32_t total) {
     if (Ef <= kNoMass || Eb <= kNoMass) return -2000;
     const long long c = (long long)Ef + Eb - total;
@@ -854,24 +869,17 @@ struct Chunk {
         }
     }
 
-    // One exponent for the lane's masses and those that may reach it; whether their spread is within bounds.
+    // One exponent for the lane's masses and those that may reach it, and that of the lane which they come from.
     template <bool UP>
-    __device__ static bool window(const Mass (&b)[K], const Mass (&l)[K], int32_t* E, int32_t* beside) {
-        int32_t top = kNoMass, low = -kNoMass;
+    __device__ static void window(const Mass (&b)[K], const Mass (&l)[K], int32_t* E, int32_t* beside) {
+        int32_t top = kNoMass;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            top = max(top, max(b[k].e, l[k].e));
-            low = min(low, min(b[k].e == kNoMass ? -kNoMass : b[k].e, l[k].e == kNoMass ? -kNoMass : l[k].e));
-        }
-        int32_t m = top, n = low;
+        for (int k = 0; k < K; ++k) top = max(top, max(b[k].e, l[k].e));
+        int32_t m = top;
 #pragma unroll
-        for (int d = 0; d < (R + K - 1) / K; ++d) {
-            m = max(UP ? from_below(m, kNoMass) : from_above(m, kNoMass), top);
-            n = min(UP ? from_below(n, -kNoMass) : from_above(n, -kNoMass), low);
-        }
+        for (int d = 0; d < (R + K - 1) / K; ++d) m = max(UP ? from_below(m, kNoMass) : from_above(m, kNoMass), top);
         *E = m;
         *beside = UP ? from_below(m, kNoMass) : from_above(m, kNoMass);
-        return m == kNoMass || m - n <= 1017 - 58 * R;
     }
 
     // One frame forwards / the bracket of one frame backwards, with aligned exponents.
@@ -959,7 +967,7 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
         bool near = true;
         for (int32_t f = wave; f < nf; f += kWaves) {
             const float lp = value_at(from.rows + (int64_t)(t0 + f) * from.frame_bytes, min(lane, x.V - 1), x.type);
-            near &= lp >= kLeastNear && lp <= kMostNear;
+            near &= lp <= kMostNear;
             table[f * kTabulated + lane] = exp_any(lp);
         }
         const bool out_of_range = __syncthreads_or(!near);
@@ -989,10 +997,10 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                 own[k] = one ? i <= y.L : i >= c * kStep && i < (c + 1) * kStep && i <= y.L;
             }
             int32_t Ef, Eb, below, above;
-            bool fine = Chunk<K, R>::template window<true>(z.fb, z.fl, &Ef, &below);
-            fine &= Chunk<K, R>::template window<false>(z.bb, z.bl, &Eb, &above);
+            Chunk<K, R>::template window<true>(z.fb, z.fl, &Ef, &below);
+            Chunk<K, R>::template window<false>(z.bb, z.bl, &Eb, &above);
             const int32_t shift = share_shift(Ef, Eb, total_e);
-            fine &= shift <= kMostShift && nf == R;
+            bool fine = shift <= kMostShift && nf == R;
             // emissions
             uint32_t raw[TABLE ? 1 : R][K], raw_blank = 0;
             if constexpr (!TABLE) {
@@ -1006,15 +1014,11 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                 }
                 const char* row = from.rows + (int64_t)(t0 + min((int32_t)(lane & (R - 1)), nf - 1)) * from.frame_bytes;
                 raw_blank = x.type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, 0) : raw_at<FLTOP_TYPE_F16>(row, 0);
-                float most_lp = raw_value(raw_blank, x.type), least_lp = most_lp;
+                fine &= raw_value(raw_blank, x.type) <= kMostNear;
 #pragma unroll
                 for (int f = 0; f < R; ++f)
 #pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        most_lp = fmaxf(most_lp, raw_value(raw[f][k], x.type));
-                        least_lp = fminf(least_lp, raw_value(raw[f][k], x.type));
-                    }
-                fine &= least_lp >= kLeastNear && most_lp <= kMostNear;
+                    for (int k = 0; k < K; ++k) fine &= raw_value(raw[f][k], x.type) <= kMostNear;
             } else {
                 fine &= !wide;
             }
@@ -1022,13 +1026,13 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
             if (__all(fine)) {
                 double p[TABLE ? 1 : R][K], pb[TABLE ? 1 : R];   // (a table is read again)
                 double blank_by_lane = 0.0;
-                if constexpr (!TABLE) blank_by_lane = exp_near(raw_value(raw_blank, x.type));
+                if constexpr (!TABLE) blank_by_lane = exp_any(raw_value(raw_blank, x.type));
                 if constexpr (!TABLE) {
 #pragma unroll
                     for (int f = 0; f < R; ++f) {
                         pb[f] = from_lane(blank_by_lane, f);
 #pragma unroll
-                        for (int k = 0; k < K; ++k) p[f][k] = exp_near(raw_value(raw[f][k], x.type));
+                        for (int k = 0; k < K; ++k) p[f][k] = exp_any(raw_value(raw[f][k], x.type));
                     }
                 }
                 auto blank_p = [&](int f) { return TABLE ? table[f * kTabulated] : pb[TABLE ? 0 : f]; };
@@ -1043,8 +1047,7 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                     ub[k] = ldexp(z.bb[k].m, z.bb[k].e - Eb);
                     ul[k] = ldexp(z.bl[k].m, z.bl[k].e - Eb);
                 }
-#pragma unroll
-                for (int f = 0; f < R; ++f) {
+                auto forward = [&](int f) {
                     const double moved = from_below(xl[K - 1], 0.0);
 #pragma unroll
                     for (int k = K - 1; k >= 0; --k) {
@@ -1055,10 +1058,9 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                         kb[f][k] = xb[k] = on * blank_p(f);
                         kl[f][k] = xl[k] = l * token_p(f, k);
                     }
-                }
+                };
                 const double factor = shift < -1000 ? 0.0 : power_of_two(min(shift, kMostShift));
-#pragma unroll
-                for (int f = R - 1; f >= 0; --f) {
+                auto backward = [&](int f) {
                     const double up_b = from_above(ub[0]), up_l = from_above(ul[0]);
                     blanks[f] = 0.0;
 #pragma unroll
@@ -1076,7 +1078,11 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                         ub[k] = blank * blank_p(f);
                         ul[k] = token * token_p(f, k);
                     }
-                }
+                };
+#pragma unroll
+                for (int f = 0; f < R; ++f) forward(f);
+#pragma unroll
+                for (int f = R - 1; f >= 0; --f) backward(f);
             } else {
                 Mass ub[K], ul[K];
 #pragma unroll
