@@ -88,6 +88,11 @@ __device__ inline double from_lane(double x, int lane) {
 __device__ inline double power_of_two(int32_t e) { return from_words((e + 1023) << 20, 0); }
 // 2^e as a factor of masses of which those that leave the range are 0.
 __device__ inline double rescaling(int32_t e) { return power_of_two(max(min(e, 1000), -1023)); }
+// x, or 0 with a mask of 0 (no branch).
+__device__ inline double masked(double x, int32_t mask) {
+    const long long a = __double_as_longlong(x);
+    return from_words((int32_t)(a >> 32) & mask, (int32_t)a & mask);
+}
 __device__ inline uint32_t high_word(double x) { return (uint32_t)(__double_as_longlong(x) >> 32); }
 
 // Emissions that a block may have to be gone through with one exponent for each lane.
@@ -154,15 +159,18 @@ struct Source {
     int32_t type, V;
 };
 
-// Rows of a block in the order in which a direction takes them; behind its nf frames the last one again.
-struct Rows {
-    const char* row;
-    int64_t step;
-    int32_t left;
-    __device__ Rows(const Source& from, int32_t t0, int32_t nf, bool reversed)
-        : row(from.rows + (int64_t)(reversed ? t0 + nf - 1 : t0) * from.frame_bytes),
-          step(reversed ? -from.frame_bytes : from.frame_bytes), left(nf - 1) {}
-    __device__ void next() { row += left-- > 0 ? step : 0; }
+// A block's frames in the order in which a direction takes them.  Behind the end of an utterance that ends within the
+// block lie frames in which the blank has probability 1 and all else 0: they leave every alignment's probability as
+// it is, and stand where the backward direction begins.
+template <int R>
+struct Span {
+    int32_t t0, end;
+    bool reversed;
+    __device__ int32_t frame(int f) const { return reversed ? t0 + R - 1 - f : t0 + f; }
+    __device__ bool real(int f) const { return frame(f) < end; }
+    __device__ const char* row(const Source& from, int f) const {   // of one behind the end, the last one
+        return from.rows + (int64_t)min(frame(f), end - 1) * from.frame_bytes;
+    }
 };
 
 // What the wavefront above needs of a block: the last lane's token mass before each frame.  (Below the first
@@ -259,22 +267,22 @@ struct Lane {
     __device__ Mass blank_mass(int k) const { return normalized(xb[k], common ? E : eb[k]); }
     __device__ Mass token_mass(int k) const { return normalized(xl[k], common ? E : el[k]); }
 
-    // Asks for the emissions of frames t0 .. t0 + nf - 1, in the order in which they are taken.
+    // Asks for a block's emissions.
     template <int TYPE>
-    __device__ void ask_as(const Source& from, int32_t t0, int32_t nf, bool reversed) {
-        Rows rows(from, t0, nf, reversed);
+    __device__ void ask_as(const Source& from, const Span<R>& span) {
 #pragma unroll
-        for (int f = 0; f < R; ++f, rows.next())
+        for (int f = 0; f < R; ++f) {
+            const char* row = span.row(from, f);
 #pragma unroll
-            for (int k = 0; k < K; ++k) raw[TABLE ? 0 : f][k] = raw_at<TYPE>(rows.row, tok[k]);
-        const int32_t g = min((int32_t)(threadIdx.x & (R - 1)), nf - 1);
-        raw_blank = raw_at<TYPE>(from.rows + (int64_t)(t0 + (reversed ? nf - 1 - g : g)) * from.frame_bytes, 0);
+            for (int k = 0; k < K; ++k) raw[TABLE ? 0 : f][k] = raw_at<TYPE>(row, tok[k]);
+        }
+        raw_blank = raw_at<TYPE>(span.row(from, threadIdx.x & (R - 1)), 0);
     }
-    __device__ void ask(const Source& from, int32_t t0, int32_t nf, bool reversed) {
+    __device__ void ask(const Source& from, const Span<R>& span) {
         if (from.type == FLTOP_TYPE_F32)
-            ask_as<FLTOP_TYPE_F32>(from, t0, nf, reversed);
+            ask_as<FLTOP_TYPE_F32>(from, span);
         else
-            ask_as<FLTOP_TYPE_F16>(from, t0, nf, reversed);   // 16 bits of either kind
+            ask_as<FLTOP_TYPE_F16>(from, span);   // 16 bits of either kind
     }
     template <int TYPE>
     __device__ void got_as() {
@@ -294,13 +302,14 @@ struct Lane {
     }
 
     // Whether this lane's emissions of the block are in range.
-    __device__ bool in_range(const double* table) const {
+    __device__ bool in_range(const double* table, const Span<R>& span) const {
         if constexpr (TABLE) {
             uint32_t most = 0, least = kMostWord;
 #pragma unroll 1
             for (int f = 0; f < R; ++f)
 #pragma unroll
                 for (int k = -1; k < K; ++k) {
+                    if (!span.real(f)) break;
                     const uint32_t w = high_word(table[f * kTabulated + (k < 0 ? 0 : tok[k < 0 ? 0 : k])]);
                     most = max(most, w);
                     least = min(least, w);
@@ -411,8 +420,7 @@ template <int K, int R, bool TABLE, bool AHEAD>
 __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t q, const double* table, bool wide, const Edge<R>& in,
                                   Edge<R>& out, double* nowhere, const Source& from) {
     const int lane = threadIdx.x & (kWave - 1);
-    const int32_t t0 = q * R;
-    const int32_t nf = min(R, way.hi - t0);
+    const Span<R> span = {q * R, way.hi, way.reversed};
     constexpr bool kRead = TABLE && AHEAD;
     double blanks[kRead ? R : 1], tokens[kRead ? R : 1][K];
     if constexpr (kRead) {
@@ -432,7 +440,7 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
     }
     int32_t E, least, below;
     bool fine = z.enter(in, &E, &least, &below) && !in.aligned;
-    if (!TABLE || wide) fine &= z.in_range(table);
+    if (!TABLE || wide) fine &= z.in_range(table, span);
     const bool near = __all(fine);
     if (lane == kWave - 1) {
         out.E = E;
@@ -445,40 +453,33 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
         const double fskip = fx * z.skip[0];
         double* const edge = lane == kWave - 1 ? out.x : nowhere + lane;
         z.rescale(E);
-        auto take_frame = [&](double* edge_at, double first, double pb, auto token_p) {
-            *edge_at = z.xl[K - 1];
-            const double moved = from_below(z.xl[K - 1], first);
+        double first[R];
+#pragma unroll
+        for (int f = 0; f < R; ++f) first[f] = in.x[f];
+        double blank_by_lane = 0.0;
+        if constexpr (!TABLE) blank_by_lane = span.real(lane & (R - 1)) ? exp_near(z.given_blank) : 1.0;
+#pragma unroll
+        for (int f = 0; f < R; ++f) {
+            double pb;
+            if constexpr (TABLE)
+                pb = kRead ? blanks[kRead ? f : 0] : table[f * kTabulated];
+            else
+                pb = from_lane(blank_by_lane, f);
+            edge[f] = z.xl[K - 1];
+            const double moved = from_below(z.xl[K - 1], first[f]);
 #pragma unroll
             for (int k = K - 1; k >= 0; --k) {
                 const double prev = k > 0 ? z.xl[k > 0 ? k - 1 : 0] : moved;
                 const double stay = fma(z.xb[k], z.live[k], z.xl[k]);
                 const double l = fma(prev, k > 0 ? z.skip[k] : fskip, stay);
                 const double b = k > 0 ? z.xb[k] + prev : fma(prev, fx, z.xb[k]);
+                double p;
+                if constexpr (TABLE)
+                    p = kRead ? tokens[kRead ? f : 0][k] : table[f * kTabulated + z.tok[k]];
+                else
+                    p = masked(exp_near(z.given[TABLE ? 0 : f][k]), span.real(f) ? -1 : 0);
                 z.xb[k] = b * pb;
-                z.xl[k] = l * token_p(k);
-            }
-        };
-        if (nf == R) {
-            double first[R];
-#pragma unroll
-            for (int f = 0; f < R; ++f) first[f] = in.x[f];
-            double blank_by_lane = 0.0;
-            if constexpr (!TABLE) blank_by_lane = exp_near(z.given_blank);
-#pragma unroll
-            for (int f = 0; f < R; ++f) {
-                const double pb = kRead ? blanks[kRead ? f : 0] : TABLE ? table[f * kTabulated] : from_lane(blank_by_lane, f);
-                take_frame(edge + f, first[f], pb, [&](int k) {
-                    return kRead   ? tokens[kRead ? f : 0][k]
-                           : TABLE ? table[f * kTabulated + z.tok[k]]
-                                   : exp_near(z.given[TABLE ? 0 : f][k]);
-                });
-            }
-        } else {   // an utterance's last block, its emissions from memory once more
-#pragma unroll 1
-            for (int f = 0; f < nf; ++f) {
-                const char* row = from.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - f : f)) * from.frame_bytes;
-                take_frame(edge + f, in.x[f], exp_near(value_at(row, 0, from.type)),
-                           [&](int k) { return exp_near(value_at(row, z.tok[k], from.type)); });
+                z.xl[k] = l * p;
             }
         }
     } else {
@@ -490,8 +491,9 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
         }
         z.common = false;
 #pragma unroll 1
-        for (int f = 0; f < nf; ++f) {
-            const char* emissions = from.rows + (int64_t)(t0 + (way.reversed ? nf - 1 - f : f)) * from.frame_bytes;
+        for (int f = 0; f < R; ++f) {
+            if (!span.real(f)) continue;
+            const char* emissions = span.row(from, f);
             const Mass blank = mass_of(value_at(emissions, 0, from.type));
             const Mass first = normalized(in.x[f], in.aligned ? in.e[f] : in.E);
             if (lane == kWave - 1) {
@@ -545,9 +547,9 @@ struct Tabulator {
     template <int TYPE>
     __device__ void ask_as(const Source& from, const Way& way, int32_t q) {
         const int32_t v = min((int32_t)(threadIdx.x & (kWave - 1)), from.V - 1);
-        Rows rows(from, q * R, min(R, way.hi - q * R), way.reversed);
+        const Span<R> span = {q * R, way.hi, way.reversed};
 #pragma unroll
-        for (int f = 0; f < R; ++f, rows.next()) raw[f] = raw_at<TYPE>(rows.row, v);
+        for (int f = 0; f < R; ++f) raw[f] = raw_at<TYPE>(span.row(from, f), v);
     }
     __device__ void ask(const Source& from, const Way& way, int32_t q) {
         if (from.type == FLTOP_TYPE_F32)
@@ -556,7 +558,7 @@ struct Tabulator {
             ask_as<FLTOP_TYPE_F16>(from, way, q);
     }
     template <int TYPE>
-    __device__ void put_as(double* table, int32_t* wide) {
+    __device__ void put_as(double* table, int32_t* wide, const Span<R>& span) {
         const int lane = threadIdx.x & (kWave - 1);
         float most = raw_as<TYPE>(raw[0]), least = most;
 #pragma unroll
@@ -565,17 +567,18 @@ struct Tabulator {
             most = fmaxf(most, lp);
             least = fminf(least, lp);
             table[f * kTabulated + lane] = exp_any(lp);
+            if (!span.real(f)) table[f * kTabulated + lane] = lane == 0 ? 1.0 : 0.0;
         }
         const bool all = __all(least >= kLeastNear && most <= kMostNear);
         if (lane == 0) *wide = !all;
     }
-    __device__ void put(const Source& from, double* table, int32_t* wide) {
+    __device__ void put(const Source& from, double* table, int32_t* wide, const Span<R>& span) {
         if (from.type == FLTOP_TYPE_F32)
-            put_as<FLTOP_TYPE_F32>(table, wide);
+            put_as<FLTOP_TYPE_F32>(table, wide, span);
         else if (from.type == FLTOP_TYPE_BF16)
-            put_as<FLTOP_TYPE_BF16>(table, wide);
+            put_as<FLTOP_TYPE_BF16>(table, wide, span);
         else
-            put_as<FLTOP_TYPE_F16>(table, wide);
+            put_as<FLTOP_TYPE_F16>(table, wide, span);
     }
 };
 
@@ -586,7 +589,7 @@ __device__ inline void tabulate_all(const Way& way, const Way& other, const Sour
     Tabulator<R> even, odd;
     auto put = [&](Tabulator<R>& one, int32_t n) {
         const int slot = lds.slot(way.side, n);
-        one.put(from, lds.table(slot), lds.wide + slot);
+        one.put(from, lds.table(slot), lds.wide + slot, Span<R>{blocks[n] * R, way.hi, way.reversed});
     };
     if (blocks.count > 0) {
         even.ask(from, way, blocks[0]);
@@ -626,8 +629,7 @@ __device__ inline void take_all(Lane<K, R, TABLE>& z, const Way& way, const Way&
     }
     const Blocks<R> blocks(way, other, used);
     auto ask = [&](int32_t n) {
-        const int32_t q = blocks[n];
-        if constexpr (!TABLE) z.ask(from, q * R, min(R, way.hi - q * R), way.reversed);
+        if constexpr (!TABLE) z.ask(from, Span<R>{blocks[n] * R, way.hi, way.reversed});
     };
     const bool works = wave < used && blocks.count > 0;
     if (works) ask(0);
@@ -919,6 +921,39 @@ __device__ inline void add_share(unsigned long long* sum, double share) {
     atomicAdd(sum, (unsigned long long)a);
 }
 
+// The pairs own_first .. own_last with aligned exponents, a pair a lane so that few registers are needed, and forwards
+// once more for each frame.
+template <int R>
+__device__ inline void aligned_chunk(const Hyp& y, const ScoreSpace& ws, int64_t at, const Source& from, int32_t t0, int32_t q,
+                                     int32_t nf, int32_t own_first, int32_t own_last, int32_t total_e, double w, int32_t v0,
+                                     int32_t v1, unsigned long long* sums, int32_t width) {
+    const int lane = threadIdx.x & (kWave - 1);
+    constexpr int32_t kStep = kWave - 2 * R;
+#pragma unroll 1
+    for (int32_t c = own_first; c <= own_last; c += kStep) {
+        const Chunk<1, R> z(y, ws, at, from.V, q, c - R);
+        const bool own = z.i0 >= c && z.i0 < c + kStep && z.i0 <= own_last;
+        Mass ub[1] = {z.bb[0]}, ul[1] = {z.bl[0]};
+#pragma unroll 1
+        for (int f = nf - 1; f >= 0; --f) {
+            Mass kb[1] = {z.fb[0]}, kl[1] = {z.fl[0]};
+#pragma unroll 1
+            for (int g = 0; g <= f; ++g) z.forward(kb, kl, from.rows + (int64_t)(t0 + g) * from.frame_bytes, from.type);
+            z.bracket(ub, ul);
+            const char* row = from.rows + (int64_t)(t0 + f) * from.frame_bytes;
+            double blank = own ? ldexp(kb[0].m * ub[0].m, kb[0].e + ub[0].e - total_e) : 0.0;
+            const int32_t v = z.tok[0] - v0;
+            if (own && z.live[0] != 0.0 && (uint32_t)v < (uint32_t)(v1 - v0))
+                add_share(&sums[f * width + v], ldexp(kl[0].m * ul[0].m, kl[0].e + ul[0].e - total_e) * w);
+            const Mass pb = mass_of(value_at(row, 0, from.type)), p = mass_of(value_at(row, z.tok[0], from.type));
+            ub[0] = normalized(ub[0].m * pb.m, ub[0].e + pb.e);
+            ul[0] = normalized(ul[0].m * p.m, ul[0].e + p.e);
+            for (int o = kWave / 2; o > 0; o >>= 1) blank += __shfl_xor(blank, o, kWave);
+            if (v0 == 0 && lane == 0) add_share(&sums[f * width], blank * w);
+        }
+    }
+}
+
 template <typename T, int R, bool TABLE>
 __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel(fltop_rows x, fltop_hypotheses h,
                                                                   const double* grad_scores, ScoreSpace ws, int32_t blocks,
@@ -928,7 +963,7 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
     constexpr int kPairs = kWave * K, kStep = kPairs - 2 * R;   // of a chunk, and from one to the next
     extern __shared__ char dynamic[];
     __shared__ double of_wave[kGradThreads / kWave];
-    __shared__ int32_t wide;
+    __shared__ int32_t flags[kGradThreads / kWave];   // weights that are no numbers, emissions out of range
     // the vocabulary is taken in `parts` ranges where a block's sums would not fit
     const int32_t width = (x.V + parts - 1) / parts;
     unsigned long long* const sums = reinterpret_cast<unsigned long long*>(dynamic);   // [R][width]
@@ -938,42 +973,63 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
     const int64_t group = blockIdx.x / parts;
     const int32_t v0 = (int32_t)(blockIdx.x % parts) * width, v1 = min(v0 + width, x.V);
     const int32_t b = (int32_t)(group / blocks), q = (int32_t)(group % blocks), t0 = q * R;
-    const int32_t frames = __builtin_amdgcn_readfirstlane(min(x.lengths[b], x.T));
-    const int32_t rows = min(R, x.T - t0), nf = min(R, frames - t0);
+    const int32_t rows = min(R, x.T - t0);
     T* const out = grad + ((int64_t)b * x.T + t0) * x.V;
+    const Source from = source_of(x, b);
+    // (all of what these loads fetch is asked for before any of it is waited for)
+    const int32_t frames_raw = x.lengths[b];
+    uint32_t block_raw[TABLE ? R : 1];
+    if constexpr (TABLE) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            if (j * kWaves >= R) break;
+            const int32_t f = min(j * kWaves + wave, rows - 1), v = min(lane, x.V - 1);
+            const char* row = from.rows + (int64_t)(t0 + f) * from.frame_bytes;
+            block_raw[j] = x.type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, v) : raw_at<FLTOP_TYPE_F16>(row, v);
+        }
+    }
     double most = 0.0;
-    bool odd = false;
+    bool odd = false, near = true;
     for (int32_t n = threadIdx.x; n < h.N; n += blockDim.x) {
         const int64_t at = (int64_t)b * h.N + n;
-        if (ws.total_e[at] <= kNoMass) continue;
         const double w = fabs(grad_scores[at]);
+        if (ws.total_e[at] <= kNoMass) continue;
         odd |= !(w <= 1.7976931348623157e308);
         most = fmax(most, w);
     }
+    for (int32_t i = threadIdx.x; i < R * width; i += blockDim.x) sums[i] = 0;
+    const int32_t frames = __builtin_amdgcn_readfirstlane(min(frames_raw, x.T)), nf = min(R, frames - t0);
+    if constexpr (TABLE) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int32_t f = j * kWaves + wave;
+            if (f >= R) break;
+            const float lp = raw_value(block_raw[j], x.type);
+            near &= lp <= kMostNear || f >= nf;
+            table[f * kTabulated + lane] = f < nf ? exp_any(lp) : lane == 0 ? 1.0 : 0.0;
+        }
+    }
 #pragma unroll
     for (int o = kWave / 2; o > 0; o >>= 1) most = fmax(most, __shfl_xor(most, o, kWave));
-    if (lane == 0) of_wave[wave] = most;
-    odd = __syncthreads_or(odd);
-    for (int w = 0; w < kWaves; ++w) most = fmax(most, of_wave[w]);
+    const int32_t flag = (__any(odd) ? 1 : 0) | (__all(near) ? 0 : 2);
+    if (lane == 0) {
+        of_wave[wave] = most;
+        flags[wave] = flag;
+    }
+    __syncthreads();
+    int32_t any = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        most = fmax(most, of_wave[w]);
+        any |= flags[w];
+    }
+    odd = any & 1;
+    const bool wide = any & 2;
     if (odd || most == 0.0 || nf <= 0) {
         for (int32_t f = 0; f < rows; ++f)
             for (int32_t v = v0 + threadIdx.x; v < v1; v += blockDim.x)
                 out[(int64_t)f * x.V + v] = from_float<T>(odd && f < nf ? NAN : 0.0f);
         return;
     }
-    const Source from = source_of(x, b);
-    for (int32_t i = threadIdx.x; i < R * width; i += blockDim.x) sums[i] = 0;
-    if constexpr (TABLE) {
-        bool near = true;
-        for (int32_t f = wave; f < nf; f += kWaves) {
-            const float lp = value_at(from.rows + (int64_t)(t0 + f) * from.frame_bytes, min(lane, x.V - 1), x.type);
-            near &= lp <= kMostNear;
-            table[f * kTabulated + lane] = exp_any(lp);
-        }
-        const bool out_of_range = __syncthreads_or(!near);
-        if (threadIdx.x == 0) wide = out_of_range;
-    }
-    __syncthreads();
     int32_t task = 0;   // chunks of hypotheses, one wavefront after the other
     for (int32_t n = 0; n < h.N; ++n) {
         const int64_t at = (int64_t)b * h.N + n;
@@ -989,18 +1045,16 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
             if (task % kWaves != wave) continue;
             const int32_t first = one ? 0 : c * kStep - R;
             const Chunk<K, R> z(y, ws, at, x.V, q, first);
-            // whether this lane's pairs are the chunk's own
+            // the chunk's own pairs, and whether they are this lane's
+            const int32_t own_first = one ? 0 : c * kStep, own_last = one ? y.L : min(y.L, (c + 1) * kStep - 1);
             bool own[K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int32_t i = z.i0 + k;
-                own[k] = one ? i <= y.L : i >= c * kStep && i < (c + 1) * kStep && i <= y.L;
-            }
+            for (int k = 0; k < K; ++k) own[k] = z.i0 + k >= own_first && z.i0 + k <= own_last;
             int32_t Ef, Eb, below, above;
             Chunk<K, R>::template window<true>(z.fb, z.fl, &Ef, &below);
             Chunk<K, R>::template window<false>(z.bb, z.bl, &Eb, &above);
             const int32_t shift = share_shift(Ef, Eb, total_e);
-            bool fine = shift <= kMostShift && nf == R;
+            bool fine = shift <= kMostShift;
             // emissions
             uint32_t raw[TABLE ? 1 : R][K], raw_blank = 0;
             if constexpr (!TABLE) {
@@ -1022,17 +1076,17 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
             } else {
                 fine &= !wide;
             }
-            double blanks[R];
             if (__all(fine)) {
+                double blanks[R];
                 double p[TABLE ? 1 : R][K], pb[TABLE ? 1 : R];   // (a table is read again)
                 double blank_by_lane = 0.0;
                 if constexpr (!TABLE) blank_by_lane = exp_any(raw_value(raw_blank, x.type));
                 if constexpr (!TABLE) {
 #pragma unroll
                     for (int f = 0; f < R; ++f) {
-                        pb[f] = from_lane(blank_by_lane, f);
+                        pb[f] = f < nf ? from_lane(blank_by_lane, f) : 1.0;
 #pragma unroll
-                        for (int k = 0; k < K; ++k) p[f][k] = exp_any(raw_value(raw[f][k], x.type));
+                        for (int k = 0; k < K; ++k) p[f][k] = f < nf ? exp_any(raw_value(raw[f][k], x.type)) : 0.0;
                     }
                 }
                 auto blank_p = [&](int f) { return TABLE ? table[f * kTabulated] : pb[TABLE ? 0 : f]; };
@@ -1083,40 +1137,11 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                 for (int f = 0; f < R; ++f) forward(f);
 #pragma unroll
                 for (int f = R - 1; f >= 0; --f) backward(f);
+                const double sum = sums_by_lane<R>(blanks);
+                if (v0 == 0 && lane < nf) add_share(&sums[lane * width], sum * w);
             } else {
-                Mass ub[K], ul[K];
-#pragma unroll
-                for (int k = 0; k < K; ++k) ub[k] = z.bb[k], ul[k] = z.bl[k];
-#pragma unroll
-                for (int f = 0; f < R; ++f) blanks[f] = 0.0;
-#pragma unroll 1
-                for (int f = nf - 1; f >= 0; --f) {
-                    Mass kb[K], kl[K];   // forwards once more from the border to this frame
-#pragma unroll
-                    for (int k = 0; k < K; ++k) kb[k] = z.fb[k], kl[k] = z.fl[k];
-#pragma unroll 1
-                    for (int g = 0; g <= f; ++g)
-                        z.forward(kb, kl, from.rows + (int64_t)(t0 + g) * from.frame_bytes, x.type);
-                    z.bracket(ub, ul);
-                    const char* row = from.rows + (int64_t)(t0 + f) * from.frame_bytes;
-                    const Mass pb = mass_of(value_at(row, 0, x.type));
-                    double blank = 0.0;
-#pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        if (own[k]) blank += ldexp(kb[k].m * ub[k].m, kb[k].e + ub[k].e - total_e);
-                        const int32_t v = z.tok[k] - v0;
-                        if (own[k] && z.live[k] != 0.0 && (uint32_t)v < (uint32_t)(v1 - v0))
-                            add_share(&sums[f * width + v], ldexp(kl[k].m * ul[k].m, kl[k].e + ul[k].e - total_e) * w);
-                        const Mass p = mass_of(value_at(row, z.tok[k], x.type));
-                        ub[k] = normalized(ub[k].m * pb.m, ub[k].e + pb.e);
-                        ul[k] = normalized(ul[k].m * p.m, ul[k].e + p.e);
-                    }
-#pragma unroll
-                    for (int g = 0; g < R; ++g) blanks[g] = g == f ? blank : blanks[g];
-                }
+                aligned_chunk<R>(y, ws, at, from, t0, q, nf, own_first, own_last, total_e, w, v0, v1, sums, width);
             }
-            const double sum = sums_by_lane<R>(blanks);
-            if (v0 == 0 && lane < nf) add_share(&sums[lane * width], sum * w);
         }
     }
     __syncthreads();
