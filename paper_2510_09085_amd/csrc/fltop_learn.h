@@ -76,11 +76,24 @@ __device__ inline Mass plus(Mass a, Mass b) {
 
 constexpr int kMostWaves = 8;   // wavefronts that one direction of a lattice takes
 
-// Masses of a pair of states (a blank and the token behind it) at the border of a block of frames: b 2^eb, l 2^el.
-struct alignas(8) Mark {
-    double b, l;
-    int32_t eb, el;
+// A mass at the border of a block of frames, as it is kept for the gradient: m 2^32 cut to a whole number, and e.  Cut to
+// 32 bits a mass is off by 2^-31 of itself at most, an occupancy by 2^-30 of itself: a gradient in fp32 is rounded by 2^-24.
+struct Kept {
+    uint32_t m;
+    int32_t e;
 };
+// Those of a pair of states, a blank and the token behind it.
+struct alignas(16) Mark {
+    Kept b, l;
+};
+__device__ inline Kept kept(double x, int32_t e) {   // x 2^e; x is normal or 0
+    const uint32_t hi = (uint32_t)((uint64_t)__double_as_longlong(x) >> 32);
+    return {0x80000000u | (uint32_t)((uint64_t)__double_as_longlong(x) >> 21), hi != 0 ? e + (int32_t)(hi >> 20) - 1022 : kNoMass};
+}
+__device__ inline Mass mass_of(Kept x) {
+    const uint64_t bits = (uint64_t)(x.m & 0x7fffffffu) << 21 | 0x3fe0000000000000ull;
+    return x.e <= kNoMass ? no_mass() : Mass{__longlong_as_double((long long)bits), x.e};
+}
 
 // What fltop_ctc_score leaves for fltop_ctc_score_grad.
 struct ScoreSpace {

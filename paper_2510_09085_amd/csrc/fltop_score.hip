@@ -436,7 +436,7 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
         Mark* const to = way.marks + (int64_t)q * way.row + z.i0;
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            to[k] = {z.xb[k], z.xl[k], z.common ? z.E : z.eb[k], z.common ? z.E : z.el[k]};
+            to[k] = {kept(z.xb[k], z.common ? z.E : z.eb[k]), kept(z.xl[k], z.common ? z.E : z.el[k])};
     }
     int32_t E, least, below;
     bool fine = z.enter(in, &E, &least, &below) && !in.aligned;
@@ -864,10 +864,10 @@ struct Chunk {
             live[k] = token ? 1.0 : 0.0;
             // backwards, pair j is blank L - j and token L - 1 - j
             const Mark f = fore[min(max(i, 0), L)], u = back[min(max(L - i, 0), L)], v = back[min(max(L - 1 - i, 0), L)];
-            fb[k] = blank ? normalized(f.b, f.eb) : no_mass();
-            fl[k] = token ? normalized(f.l, f.el) : no_mass();
-            bb[k] = blank ? normalized(u.b, u.eb) : no_mass();
-            bl[k] = token ? normalized(v.l, v.el) : no_mass();
+            fb[k] = blank ? mass_of(f.b) : no_mass();
+            fl[k] = token ? mass_of(f.l) : no_mass();
+            bb[k] = blank ? mass_of(u.b) : no_mass();
+            bl[k] = token ? mass_of(v.l) : no_mass();
         }
     }
 
