@@ -819,7 +819,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
 // whole numbers: in any order the same.  The conditions for one exponent for each lane are those of the scores'
 // blocks, for both directions, and that P's exponent is within reach of theirs.
 
-constexpr int kGradPairs = 2, kGradThreads = 256;   // (fewer threads where there are fewer chunks)
+constexpr int kGradPairs = 2, kGradThreads = 256;   // (at most)
 
 __device__ inline int32_t from_above(int32_t x, int32_t last) {
     return __builtin_amdgcn_update_dpp(last, x, 0x130, 0xf, 0xf, false);  // wave_shl:1
@@ -1194,9 +1194,13 @@ hipError_t grad_as(const fltop_rows& x, const fltop_hypotheses& h, const double*
     const int32_t parts = (x.V * R * 8 + 65535) / 65536, width = (x.V + parts - 1) / parts;
     const int32_t blocks = (int32_t)blocks_of(x.T, R);
     const size_t bytes = (size_t)R * width * 8 + (TABLE ? R * kTabulated * 8 : 0);
-    // as many wavefronts as there may be chunks
+    // With a table one wavefront for six chunks: shorter hypotheses than the longest leave none idle, and the others' loads
+    // go on while one waits (64 transcripts: 40 us with a wavefront for each of 3 chunks, 28 with one for all; 256 of up to
+    // 7 chunks: 422 with four, 287 with one; 32 x 4 hypotheses: 47 with four, 42 with two, 55 with one).  Without one as many
+    // as there may be chunks, which share the block's long rows of sums (32 x 8: 212 us with one, 127 with two, 80 with four).
     const int64_t chunks = (int64_t)h.N * ((h.U + 1) / (kWave * kGradPairs - 2 * R) + 1);
-    const unsigned threads = chunks < kGradThreads / kWave ? (unsigned)chunks * kWave : kGradThreads;
+    const int64_t waves = TABLE ? chunks / 6 : chunks, most = kGradThreads / kWave;
+    const unsigned threads = kWave * (unsigned)(waves < 1 ? 1 : waves < most ? waves : most);
     hipLaunchKernelGGL((score_grad_kernel<T, R, TABLE>), dim3((unsigned)(x.B * (int64_t)blocks * parts)), dim3(threads), bytes, stream, x, h, grad_scores, ws, blocks, parts, static_cast<T*>(grad));
     return hipGetLastError();
 }
