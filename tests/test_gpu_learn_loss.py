@@ -501,3 +501,56 @@ def test_a_training_step_from_the_search(dev, call):
     p = np.exp(xs)
     want = g - p * g.sum(2, keepdims=True)
     assert np.all(np.abs(logits.grad.double().cpu().numpy() - want) <= 34 * 2.0 ** -23 * (np.abs(g).sum(2, keepdims=True) + 1e-3))
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "square"])
+@pytest.mark.parametrize("B,N,M", [(64, 32, 64), (1, 2048, 4096), (3, 683, 5), (64, 32, 65), (2, 2048, 513), (1, 1, 4096),
+                                   (4096, 1, 1), (2, 3, 5000)])
+def test_pairs_at_the_borders_of_the_launches(dev, kind, B, N, M):
+    if N > binding.MAX_BEAM:
+        N = binding.MAX_BEAM
+    rng = np.random.default_rng(B * N + M)
+    s = -100 * rng.random((B, N))
+    pairs = rng.integers(0, N, (B, M, 2)).astype(np.int32)
+    out = binding.preference_loss(*put(dev, s, pairs), kind=kind, beta=0.3, scale=2.0)
+    loss, margins, grad, used = ref.preference(s, pairs, None, None, kind, 0.3, 0.0, 2.0)
+    err = 2.0 ** -53 * 200
+    top = {"sigmoid": 0.3, "square": 2 * 100.0 + 4}[kind]
+    assert np.all(np.abs(out["margins"].cpu().numpy() - margins) <= err)
+    assert abs(float(out["loss"]) - loss) <= top * err + loss_tolerance(used, abs(loss) + 1)
+    worst = np.zeros((B, N))
+    for b in range(B):
+        np.add.at(worst[b], pairs[b].ravel(), 2.0 / used)
+    assert np.all(np.abs(out["grad_scores"].cpu().numpy() - grad) <= worst * (2 * err + loss_tolerance(2 * M, top)))
+
+
+@pytest.mark.parametrize("B", [1, 5000])
+def test_small_slopes_keep_their_digits(dev, B):
+    """Where all pairs are won by far each derivative is e^-40 of beta, and still a number of 50 bits."""
+    rng = np.random.default_rng(B)
+    s = np.stack([np.zeros(B), -400 - 20 * rng.random(B)], 1)
+    pairs = np.tile(np.array([[[0, 1]]], np.int32), (B, 1, 1))
+    got = binding.preference_loss(*put(dev, s, pairs), beta=0.1)["grad_scores"].cpu().numpy()
+    x = 0.1 * (s[:, 0] - s[:, 1])
+    want = -0.1 / (1.0 + np.exp(x)) / B
+    # beta times a margin is rounded once (42 * 2^-53 in e^x), the rest as in the other losses
+    np.testing.assert_allclose(got, np.stack([want, -want], 1), rtol=42 * 2.0 ** -53 + loss_tolerance(2, 1), atol=0)
+
+
+def test_pairs_at_an_odd_place(dev):
+    """A list of pairs need not begin at a multiple of 8 bytes."""
+    rng = np.random.default_rng(3)
+    s = -10 * rng.random((2, 5))
+    pairs = rng.integers(0, 5, (2, 6, 2)).astype(np.int32)
+    room = torch.zeros(25, dtype=torch.int32, device=dev)
+    view = room[1:].view(2, 6, 2)
+    view.copy_(torch.from_numpy(pairs))
+    S, P = put(dev, s, pairs)
+    a, b = binding.preference_loss(S, P), binding.preference_loss(S, view)
+    assert all(torch.equal(a[k], b[k]) for k in ("loss", "margins", "grad_scores"))
+
+
+@pytest.mark.parametrize("reduction", ["token", "sequence", "sum"])
+@pytest.mark.parametrize("B,N", [(1, 2048), (2, 1025), (2048, 1), (2049, 1), (31, 66), (33, 63)])
+def test_policy_at_the_borders_of_the_launches(dev, B, N, reduction):
+    test_policy(dev, reduction, B, N)

@@ -423,3 +423,69 @@ def test_places_beyond_32_bits(dev):
     got = grad[-1].double().cpu().numpy()
     assert torch.equal(grad[0], grad[-1])
     assert np.all(np.abs(got - g[0]) <= ref.grad_tolerance("f32", T, g, size, quanta * 2000)[0])
+
+
+@pytest.mark.parametrize("V", [32, 65])
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 15, 16, 17, 23, 24, 25])
+def test_ends_of_utterances_within_a_block(dev, T, V):
+    """Lengths of every remainder, hypotheses that fill them and that are empty."""
+    lengths = [T, T - 1, max(0, T - 3), max(0, T - 6), T]
+    rng = np.random.default_rng(T)
+    tl = [[0, (n + 1) // 2, rng.integers(0, T + 1)] for n in lengths]
+    check(dev, *make(T + V, 5, 3, T, V, T, lengths=lengths, token_lengths=tl, repeats=0.1))
+
+
+@pytest.mark.parametrize("V", [29, 90])
+@pytest.mark.parametrize("U", [127, 128, 383, 384, 511, 512, 767, 768, 895, 896, 959, 960])
+def test_room_at_the_borders_of_the_builds(dev, U, V):
+    """Room of U tokens, hypotheses that take all of it and less; only the room chooses how the lattice is laid out."""
+    T = U + U // 8 + 3
+    lp, ln, tok, tl, w = make(U + V, 1, 3, T, V, U, lengths=[T], token_lengths=[[U, U // 2, 3]], flat=0.5, repeats=0.02)
+    check(dev, lp, ln, tok, tl, w)
+
+
+@pytest.mark.parametrize("V", [32, 100])
+def test_many_hypotheses(dev, V):
+    """So many that workgroups of more wavefronts a compute unit are taken."""
+    check(dev, *make(V, 18, 30, 40, V, 12))
+
+
+@pytest.mark.parametrize("V", [32, 70])
+def test_rows_of_an_untrained_model(dev, V):
+    """Far from each alignment being alike: masses of neighbours lie hundreds of nats apart."""
+    rng = np.random.default_rng(V)
+    lp, ln, tok, tl, w = make(V, 2, 2, 300, V, 110, lengths=[300, 293], token_lengths=[[100, 20], [110, 1]])
+    x = rng.standard_normal(lp.shape) * 4
+    lp = (x - np.log(np.exp(x).sum(-1, keepdims=True))).astype(np.float32)
+    check(dev, lp, ln, tok, tl, w)
+
+
+@pytest.mark.parametrize("V", [12, 80])
+@pytest.mark.parametrize("shift", [9.0, 11.0, 60.0, -35.0, -60.0])
+def test_rows_that_are_not_normalised(dev, V, shift):
+    """Emissions far above 0 or far below are as good as any; the occupancies do not see a shift."""
+    lp, ln, tok, tl, w = make(V, 2, 3, 43, V, 12, lengths=[43, 40])
+    check(dev, lp + np.float32(shift), ln, tok, tl, w)
+
+
+def test_a_vocabulary_whose_sums_are_taken_in_ranges(dev):
+    lp, ln, tok, tl, w = make(77, 2, 3, 21, binding.MAX_VOCAB - 1, 9, lengths=[21, 18])
+    check(dev, lp, ln, tok, tl, w)
+
+
+def test_two_calls_at_once(dev):
+    """Two streams, each with a workspace of its own."""
+    data = [make(50 + i, 3, 4, 90 + i, 32, 20) for i in range(2)]
+    streams = [torch.cuda.Stream(dev) for _ in range(2)]
+    put = [[torch.from_numpy(np.ascontiguousarray(a)).to(dev) for a in d] for d in data]
+    alone = []
+    for x, ln, tok, tl, w in put:
+        out = binding.ctc_score(x, ln, tok, tl, want_grad=True)
+        alone.append((out["scores"], binding.ctc_score_grad(x, ln, tok, tl, w, out["workspace"])))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        outs = [binding.ctc_score(*p[:4], want_grad=True, stream=s) for p, s in zip(put, streams)]
+        grads = [binding.ctc_score_grad(*p[:5], o["workspace"], stream=s) for p, o, s in zip(put, outs, streams)]
+        torch.cuda.synchronize()
+        for (scores, grad), o, g in zip(alone, outs, grads):
+            assert torch.equal(scores, o["scores"]) and torch.equal(grad, g)
