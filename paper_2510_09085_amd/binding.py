@@ -576,7 +576,7 @@ def ctc_score(logprobs: torch.Tensor, lengths: torch.Tensor, tokens: torch.Tenso
     transposed is fine), lengths [B]; tokens [B,N,U] and token_lengths [B,N] int32 as decode's
     n-best export gives them (slices too: `nbest_tokens[:, :8, :200]`), counts [B] its nbest_count.
     Returns scores [B,N] float64; with want_grad also the workspace that ctc_score_grad needs
-    (about 6 * B * N * T * U bytes: slice the tokens to the longest hypothesis)."""
+    (about 4 * B * N * T * U bytes: slice the tokens to the longest hypothesis)."""
     x = _rows(logprobs, lengths, "logprobs")
     dev = logprobs.device
     h = _hypotheses(tokens, token_lengths, counts, x.B, dev)

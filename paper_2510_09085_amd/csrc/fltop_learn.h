@@ -74,7 +74,7 @@ __device__ inline Mass plus(Mass a, Mass b) {
     return {ldexp(a.m, a.e - e) + ldexp(b.m, b.e - e), e};  // not normalized
 }
 
-constexpr int kMostWaves = 8;   // wavefronts that one direction of a lattice takes
+constexpr int kMostWaves = 16;   // wavefronts that one direction of a lattice takes
 
 // A mass at the border of a block of frames, as it is kept for the gradient: m 2^32 cut to a whole number, and e.  Cut to
 // 32 bits a mass is off by 2^-31 of itself at most, an occupancy by 2^-30 of itself: a gradient in fp32 is rounded by 2^-24.
@@ -105,8 +105,10 @@ struct ScoreSpace {
     size_t bytes;
 };
 
-// Pairs of states that a lane holds: two while a direction, and a wavefront that tabulates for it, have eight at most.
-inline int lattice_pairs(int32_t U) { return U < 896 ? 2 : U < 1024 ? 4 : 8; }
+// Pairs of states that a lane holds where a direction has a workgroup of its own: two while that has sixteen wavefronts at
+// most, with the one that tabulates.  (With eight pairs the registers spill: 16 transcripts of 1700 tokens over 3600 frames
+// took 12.5 ms, both directions at once, and take 5.7 ms now.)
+inline int lattice_pairs(int32_t U) { return U < 1920 ? 2 : 4; }
 inline int waves_for(int32_t U, int pairs) { return (U + 64 * pairs) / (64 * pairs); }   // for U + 1 pairs
 // Frames that are gone through together: exponents are kept once for each such block.
 inline int block_frames(int pairs) { return pairs < 4 ? 8 : 4; }

@@ -3,7 +3,7 @@
 // are, and there are few of them.
 //
 // A mean over what takes part needs its number before the gradient.  Small batches are one workgroup's, in one launch (64
-// pairs: 7.5 us, nearly all of it latency, where two launches took 10).
+// pairs: 7.5 us, nearly all of it latency; two launches, as over 256 x 32 scores of a policy, take 10.5 between them).
 // Else one workgroup per utterance sums its own values, counts them and leaves the gradient unscaled; a second kernel adds
 // the utterances' sums up (each of its workgroups all of them, in one order) and scales.
 //

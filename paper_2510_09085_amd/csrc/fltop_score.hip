@@ -37,12 +37,15 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 
 // ---- how a hypothesis is laid out over the lanes -------------------------------------------------
 //
-// A workgroup takes one hypothesis, forwards and backwards at once: W wavefronts for each direction,
-// lane by lane K pairs (b_i, l_i) each.  For the score alone both directions go to the middle of the
-// utterance: half as many serial frames as one direction would have.  With a gradient wanted both go
-// all the way and leave their masses at the borders of the blocks (below); a second kernel then goes
-// through the blocks of all utterances at once, once more from either border, and needs no masses of
-// single frames in memory.
+// W wavefronts take a direction of a hypothesis, lane by lane K pairs (b_i, l_i) each.  For the score alone one workgroup
+// takes both directions to the middle of the utterance: half as many serial frames as one direction would have.  With a
+// gradient wanted each direction has a workgroup, goes all the way and leaves its masses at the borders of the blocks
+// (below); a second kernel then goes through the blocks of all utterances at once, once more from either border, and needs
+// no masses of single frames in memory.
+//
+// The serial frames bound it: 64 transcripts of 500 frames take 79 us, 63 blocks at about 1.2 us each, of which the five
+// products and sums of a frame's two pairs are a third; the rest are the latencies of the barrier, of LDS, of the lanes'
+// exponents and of the shifts.  2048 hypotheses of 500 frames keep all compute units busy and take 270 us.
 //
 // Frames come in blocks of R.  Within a block only l_{i-1} passes from lane to lane (one DPP shift),
 // and the wavefront above takes the same block one turn later with the last lane's masses from LDS,
@@ -55,8 +58,8 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 //   - no emission needed in the block is below 2^-58 (e^-40) or from 2^14 up,
 // then nothing leaves the range of fp64: masses stay above 2^(E - kSpread - 58 R) and below 2^(E + 128)
 // until its end.  Of the lanes below a lane whose states all have mass only that lane's own count: what
-// reaches it and leaves fp64 is below 2^-1022 of E, where each sum has a term of its own of 2^-957 at least
-// (K = 2), so that nothing of 64 bits is lost.  A frame is then three multiply-adds and two products for each
+// reaches it and leaves fp64 is below 2^-1022 of E, where each sum has a term of its own of 2^-957 at
+// least, so that nothing of 64 bits is lost.  A frame is then three multiply-adds and two products for each
 // pair.  Blocks that do not hold this (masks of -inf, masses of e^-3000 that may be needed yet) are gone
 // through with aligned exponents.  Rows of a trained model stay within: 10 tokens at e^-25 are 360 bits.
 //
@@ -686,42 +689,44 @@ struct Role {
     __device__ int32_t first_pair() const { return (wave * kWave + lane) * K; }
 };
 
-// Scores, both directions of a hypothesis in a workgroup.  With KEEP each in one of its own: scores by the forward one, and
-// the masses at the borders of blocks by both.
-template <int K, int R, int WAVES, int THREADS, bool TABLE, bool KEEP>
+// Scores, both directions of a hypothesis in a workgroup.  With ONE, a direction: scores by the forward one, all the way;
+// where a gradient is wanted (`ws`), the backward one has a workgroup too, and both leave the masses at the borders of
+// blocks.
+template <int K, int R, int WAVES, int THREADS, bool TABLE, bool ONE>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))) void score_kernel(
     fltop_rows x, fltop_hypotheses h, double* out_scores, ScoreSpace ws) {
-    constexpr int kSides = KEEP ? 1 : 2;
+    constexpr int kSides = ONE ? 1 : 2;
     extern __shared__ char dynamic[];
     __shared__ Mass sums[kMostWaves];
     __shared__ Mass last[kMostWaves];
-    const int64_t at = KEEP ? blockIdx.x / 2 : blockIdx.x;
+    const bool keep = ONE && ws.marks != nullptr;
+    const int64_t at = keep ? blockIdx.x / 2 : blockIdx.x;
     const int32_t b = (int32_t)(at / h.N), n = (int32_t)(at % h.N);
     const Hyp y = hypothesis(x, h, b, n);
     const Role<K, TABLE, kSides> role;
     const Lds<R, TABLE, kSides> lds(dynamic, role.W, h.U);
-    const bool reversed = KEEP ? blockIdx.x % 2 : role.side;
+    const bool reversed = keep ? blockIdx.x % 2 : role.side;
     Lane<K, R, TABLE> z;
     // (the lanes of a wavefront that tabulates lie behind the last pair)
     const bool fine = y.L >= 0 && z.start(y, x.V, reversed, role.tabulates ? y.L + 1 : role.first_pair());
     if (__syncthreads_or(!fine)) {
-        if (threadIdx.x == 0 && !(KEEP && reversed)) {
+        if (threadIdx.x == 0 && !(ONE && reversed)) {
             out_scores[at] = y.L == -2 ? NAN : -INFINITY;
-            if (KEEP) ws.total_m[at] = 0.0, ws.total_e[at] = kNoMass;
+            if (keep) ws.total_m[at] = 0.0, ws.total_e[at] = kNoMass;
         }
         return;
     }
     const int32_t used = y.L / (kWave * K) + 1;
     const int32_t middle = middle_of<R>(y.frames);
-    const Way way = {!KEEP && reversed ? middle : 0, KEEP || reversed ? y.frames : middle, reversed, role.side,
-                     KEEP ? ws.marks + (at * 2 + reversed) * ws.marks_of : nullptr, (int32_t)ws.row};
-    const Way other = KEEP ? way : Way{reversed ? 0 : middle, reversed ? middle : y.frames, !reversed, 1 - role.side, nullptr, 0};
+    const Way way = {!ONE && reversed ? middle : 0, ONE || reversed ? y.frames : middle, reversed, role.side,
+                     keep ? ws.marks + (at * 2 + reversed) * ws.marks_of : nullptr, (int32_t)ws.row};
+    const Way other = ONE ? way : Way{reversed ? 0 : middle, reversed ? middle : y.frames, !reversed, 1 - role.side, nullptr, 0};
     if (role.tabulates) {
         if constexpr (TABLE) tabulate_all<R, kSides>(way, other, source_of(x, b), used, lds);
     } else {
         take_all<K, R, TABLE, K == 2 && WAVES == 3, kSides>(z, way, other, source_of(x, b), role.wave, used, lds);
     }
-    if constexpr (KEEP) {
+    if constexpr (ONE) {
         // P = b_L + l_{L-1} after the last frame
         if (reversed) return;
         if (!role.tabulates) {
@@ -741,8 +746,10 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
             Mass p = y.L % K != 0 || y.L == 0 ? sums[0] : plus(sums[0], sums[1]);
             p = normalized(p.m, p.e);
             out_scores[at] = ln_of(p);
-            ws.total_m[at] = p.m;
-            ws.total_e[at] = p.e;
+            if (keep) {
+                ws.total_m[at] = p.m;
+                ws.total_e[at] = p.e;
+            }
         }
         return;
     }
@@ -816,8 +823,11 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
 // of kWave K pairs: forwards from the masses at the block's lower border, with the masses after each frame in registers;
 // then backwards from those at the upper border, both in the same lanes.  Within a block a mass goes R pairs far, so
 // chunks that overlap by 2 R pairs need nothing from each other.  Occupancies are added to rows of V sums in LDS, as
-// whole numbers: in any order the same.  The conditions for one exponent for each lane are those of the scores'
-// blocks, for both directions, and that P's exponent is within reach of theirs.
+// whole numbers: in any order the same.  One exponent for each lane does wherever P's is within reach of it (kMostShift).
+//
+// About a thousand vector instructions a chunk and block, and loads of the borders that depend on the hypothesis's length,
+// which is loaded before: 64 transcripts of 500 frames take 28 us, 256 of up to 1500 frames 290 us, where the borders'
+// 0.6 GB alone are 120 us.  Four wavefronts a SIMD, the most that registers allow, are worth more than a few spills.
 
 constexpr int kGradPairs = 2, kGradThreads = 256;   // (at most)
 
@@ -1151,40 +1161,36 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
                 from_float<T>(f < nf ? (float)((double)(long long)sums[f * width + v - v0] * (most / kOne)) : 0.0f);
 }
 
-// Pairs of a lane, frames of a block, most threads.
-template <int K, int R, int WAVES, bool TABLE>
-struct Build {
-    // (as many wavefronts as U can need: of 2 pairs 7 or 4, of 4 pairs 4, of 8 pairs 8; and the one that tabulates)
-    static constexpr int kMost = (K == 2 && WAVES == 4 ? 7 : K < 8 ? 4 : 8) + (TABLE ? 1 : 0);
-    static hipError_t score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
-                            hipStream_t stream) {
-        const int W = waves_for(h.U, K), threads = kWave * (TABLE ? W + 1 : W);
-        const unsigned hyps = (unsigned)(x.B * h.N);
-        if (keep)
-            hipLaunchKernelGGL((score_kernel<K, R, WAVES, kWave * kMost, TABLE, true>), dim3(2 * hyps), dim3(threads),
-                               (Lds<R, TABLE, 1>::bytes(W, h.U)), stream, x, h, out_scores, *keep);
-        else
-            hipLaunchKernelGGL((score_kernel<K, R, WAVES, 2 * kWave * kMost, TABLE, false>), dim3(hyps), dim3(2 * threads),
-                               (Lds<R, TABLE, 2>::bytes(W, h.U)), stream, x, h, out_scores, ScoreSpace{});
-        return hipGetLastError();
-    }
-};
+// Pairs of a lane, wavefronts of a direction (at most), frames of a block, wavefronts a SIMD has registers for.
+template <int K, int MOST, int R, int WAVES, bool TABLE, bool ONE>
+hipError_t score_with(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
+                      hipStream_t stream) {
+    constexpr int kSides = ONE ? 1 : 2, kThreads = kWave * kSides * (MOST + (TABLE ? 1 : 0));
+    const int W = waves_for(h.U, K);
+    const unsigned hyps = (unsigned)(x.B * h.N), threads = kWave * kSides * (TABLE ? W + 1 : W);
+    const size_t bytes = Lds<R, TABLE, kSides>::bytes(W, h.U);
+    hipLaunchKernelGGL((score_kernel<K, R, WAVES, kThreads, TABLE, ONE>), dim3(keep ? 2 * hyps : hyps), dim3(threads), bytes,
+                       stream, x, h, out_scores, keep ? *keep : ScoreSpace{});
+    return hipGetLastError();
+}
 
-// Calls `f` with the build for these shapes.
-template <typename F>
-hipError_t with_build(const fltop_rows& x, const fltop_hypotheses& h, F f) {
-    const bool table = x.V <= kTabulated;
-    switch (lattice_pairs(h.U)) {
-        case 2:
-            // Registers for three wavefronts a SIMD, without spills, where a direction has four at most and the hypotheses do
-            // not fill the chip twice (64 transcripts of 229 tokens: 104 us, 128 with the other build); else for four, of up to
-            // seven a direction (2048 hypotheses of 229: 300 us, 384 with the first).
-            if (h.U < 512 && (int64_t)x.B * h.N < 512)
-                return table ? f(Build<2, 8, 3, true>{}) : f(Build<2, 8, 3, false>{});
-            return table ? f(Build<2, 8, 4, true>{}) : f(Build<2, 8, 4, false>{});
-        case 4: return table ? f(Build<4, 4, 3, true>{}) : f(Build<4, 4, 3, false>{});
-        default: return f(Build<8, 4, 4, false>{});
+template <bool TABLE>
+hipError_t score_as(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
+                    hipStream_t stream) {
+    // Registers for three wavefronts a SIMD, so that a table's exponentials can be read ahead, where a direction has four at
+    // most and the hypotheses do not fill the chip twice (64 transcripts of 229 tokens: 79 us, 86 with the other build); else
+    // for four (2048 hypotheses of 229: 269 us, 345 with the first).
+    const bool few = h.U < 512 && (int64_t)x.B * h.N < 512;
+    if (!keep && h.U < 896) {
+        if (few) return score_with<2, 4, 8, 3, TABLE, false>(x, h, out_scores, keep, stream);
+        return score_with<2, 7, 8, 4, TABLE, false>(x, h, out_scores, keep, stream);
     }
+    // Two directions in a workgroup have no place for more than 1024 pairs of two a lane, so four (16 transcripts of 1000
+    // tokens over 2400 frames: 0.9 ms, 2.5 ms with one direction all the way); longer ones go one way.
+    if (!keep && h.U < 1024) return score_with<4, 4, 4, 3, TABLE, false>(x, h, out_scores, keep, stream);
+    if (lattice_pairs(h.U) == 4) return score_with<4, 16, 4, 4, false, true>(x, h, out_scores, keep, stream);
+    if (few) return score_with<2, 4, 8, 3, TABLE, true>(x, h, out_scores, keep, stream);
+    return score_with<2, 15, 8, 4, TABLE, true>(x, h, out_scores, keep, stream);
 }
 
 template <typename T, int R, bool TABLE>
@@ -1220,7 +1226,8 @@ hipError_t grad_of(const fltop_rows& x, const fltop_hypotheses& h, const double*
 
 hipError_t launch_score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores, const ScoreSpace* keep,
                         hipStream_t stream) {
-    return with_build(x, h, [&](auto build) { return decltype(build)::score(x, h, out_scores, keep, stream); });
+    return x.V <= kTabulated ? score_as<true>(x, h, out_scores, keep, stream)
+                             : score_as<false>(x, h, out_scores, keep, stream);
 }
 
 hipError_t launch_score_grad(const fltop_rows& x, const fltop_hypotheses& h, const double* grad_scores,

@@ -404,9 +404,9 @@ def test_pruned_search_bounds_from_below(dev):
 
 
 def test_places_beyond_32_bits(dev):
-    """More than 2^32 bytes of lattice: the last hypotheses are as good as the first."""
-    B, N, T, U, V = 48, 32, 1400, 1100, 8
-    assert binding.score_workspace_bytes(B, T, N, U) > 2 ** 34
+    """More than 2^31 kept pairs of states, 16 bytes each: the last hypotheses are as good as the first."""
+    B, N, T, U, V = 112, 32, 1400, 1900, 8
+    assert binding.score_workspace_bytes(B, T, N, U) > 2 ** 35
     lp, ln, tok, tl, w = make(22, 1, 1, T, V, 30, lengths=[T], token_lengths=[[30]])
     x = torch.from_numpy(lp).to(dev).expand(B, T, V)
     tokens = torch.zeros((B, N, U), dtype=torch.int32, device=dev)
