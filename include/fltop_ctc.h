@@ -331,8 +331,8 @@ typedef struct fltop_hypotheses {
  *   workspace  NULL if only the scores are wanted; else dev, 256-byte aligned, of at least
  *              fltop_ctc_score_workspace_bytes(B, T, N, U) bytes, into which the call puts what
  *              fltop_ctc_score_grad goes on from.
- * Refused: B, T, N < 1, V < 2, U < 1 or beyond FLTOP_MAX_LABELS, B * N or B * T >= 2^31
- * (BAD_SHAPE), N > FLTOP_MAX_BEAM (BAD_BEAM), V > FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type
+ * Refused: B, T, N < 1, V < 2, U < 1 or beyond FLTOP_MAX_LABELS, B >= 2^24, B * N >= 2^21 or
+ * B * T >= 2^31, with a workspace B * (T / 8 + 1) >= 2^22 too (BAD_SHAPE), N > FLTOP_MAX_BEAM (BAD_BEAM), V > FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type
  * (BAD_OPTION). */
 size_t fltop_ctc_score_workspace_bytes(int32_t B, int32_t T, int32_t N, int32_t U);
 int fltop_ctc_score(const fltop_rows* logprobs, const fltop_hypotheses* hyps, double* out_scores,
@@ -359,8 +359,9 @@ int fltop_ctc_score_grad(const fltop_rows* logprobs, const fltop_hypotheses* hyp
  *     FLTOP_PREFERENCE_HINGE    max(0, 1 - beta h)
  *     FLTOP_PREFERENCE_SQUARE   (h - 1 / (2 beta))^2
  * The result is the mean over the pairs that take part: those before pair_counts[b] whose two
- * indices are in [0,N), whose scores are all finite and whose margin is.  A pair may appear twice (it counts
- * twice) and hypotheses may be shared by pairs (their gradients add up).  No pair: loss 0. */
+ * indices are in [0,N), whose scores are all finite and whose margin is.  A pair may appear
+ * twice (it counts twice) and hypotheses may be shared by pairs (their gradients add up).  No
+ * pair: loss 0. */
 #define FLTOP_PREFERENCE_SIGMOID 0
 #define FLTOP_PREFERENCE_HINGE   1
 #define FLTOP_PREFERENCE_SQUARE  2
@@ -369,7 +370,7 @@ typedef struct fltop_preference {
     const double*  ref_scores;    /* dev [B,N] or NULL                                            */
     const int32_t* pairs;         /* dev [B,M,2] (won, lost)                                      */
     const int32_t* pair_counts;   /* dev [B] (clamped to [0,M]) or NULL for M each                */
-    int32_t        B, N, M;       /* N up to FLTOP_MAX_BEAM                                       */
+    int32_t        B, N, M;       /* B < 2^24, N up to FLTOP_MAX_BEAM, M up to 2^29               */
     int32_t        kind;          /* FLTOP_PREFERENCE_*                                           */
     double         beta;          /* > 0                                                          */
     double         label_smoothing; /* [0, 0.5], sigmoid only (else 0)                            */
@@ -403,7 +404,7 @@ typedef struct fltop_policy {
 size_t fltop_policy_workspace_bytes(int32_t B, int32_t T);
 
 /* The loss over log-probabilities that the caller has (hypotheses: fltop_ctc_score's [B,N]):
- *   scores, old_scores, ref_scores (or NULL), advantages   dev [B,N]
+ *   scores, old_scores, ref_scores (or NULL), advantages   dev [B,N], B < 2^24
  *   counts       dev [B] entries of row b (clamped to [0,N]) or NULL
  *   summary      dev [3]: loss, kl (reduced alike), share of entries whose ratio was clipped
  *   grad_scores  dev [B,N], 0 for entries that take no part

@@ -6,24 +6,29 @@
 
 namespace {
 
+// A launch has fewer than 2^32 threads: of 256 in a workgroup for each row of a batch, of 1024 in two workgroups for each
+// hypothesis, of 256 in four for each block of frames.
+constexpr int64_t kMostBatch = (1 << 24) - 1, kMostHypotheses = (1 << 21) - 1, kMostBlocks = (1 << 22) - 1;
+
 int check_rows(const fltop_rows* x, bool decodes) {
     if (!x || !x->data || !x->lengths) return FLTOP_ERR_NULL_POINTER;
     if (x->B < 1 || x->T < 1 || x->V < (decodes ? 2 : 1)) return FLTOP_ERR_BAD_SHAPE;
     if (x->batch_stride < 0 || x->frame_stride < 0) return FLTOP_ERR_BAD_SHAPE;
-    // a workgroup for each frame
-    if ((int64_t)x->B * x->T > (int64_t)INT32_MAX) return FLTOP_ERR_BAD_SHAPE;
+    if (x->B > kMostBatch || (int64_t)x->B * x->T > (int64_t)INT32_MAX) return FLTOP_ERR_BAD_SHAPE;
     if (decodes && x->V > FLTOP_MAX_VOCAB) return FLTOP_ERR_VOCAB_TOO_BIG;
     if (x->type < FLTOP_TYPE_F32 || x->type > FLTOP_TYPE_F16) return FLTOP_ERR_BAD_OPTION;
     return FLTOP_OK;
 }
 
 bool lattice_shapes(int32_t B, int32_t T, int32_t N, int32_t U) {
-    return B >= 1 && T >= 1 && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 && U <= FLTOP_MAX_LABELS && (int64_t)B * N <= (int64_t)INT32_MAX;
+    return B >= 1 && T >= 1 && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 && U <= FLTOP_MAX_LABELS &&
+           (int64_t)B * N <= kMostHypotheses;
 }
 
-// Whether the lattices of these shapes can be addressed (their places as bytes within 63 bits).
+// Whether the borders of these lattices can be addressed (their places as bytes within 63 bits), and their blocks launched.
 bool lattice_fits(int32_t B, int32_t T, int32_t N, int32_t U) {
-    return lattice_shapes(B, T, N, U) && (double)B * N * T * (2.0 * U + 1100.0) < 7e16;
+    return lattice_shapes(B, T, N, U) && (int64_t)B * (T / 8 + 1) <= kMostBlocks &&
+           (double)B * N * T * (2.0 * U + 1100.0) < 7e16;
 }
 
 int check_hypotheses(const fltop_rows* x, const fltop_hypotheses* h) {
@@ -89,13 +94,13 @@ extern "C" int fltop_ctc_score_grad(const fltop_rows* logprobs, const fltop_hypo
 }
 
 extern "C" size_t fltop_preference_workspace_bytes(int32_t B) {
-    return B < 1 ? 0 : fltop::align_up((size_t)B * 2 * sizeof(double), 256);
+    return B < 1 || B > kMostBatch ? 0 : fltop::align_up((size_t)B * 2 * sizeof(double), 256);
 }
 
 extern "C" int fltop_preference_loss(const fltop_preference* p, void* workspace, size_t workspace_bytes,
                                      void* hip_stream) {
     if (!p || !p->scores || !p->pairs || !p->loss || !p->margins || !p->grad_scores) return FLTOP_ERR_NULL_POINTER;
-    if (p->B < 1 || p->N < 1 || p->M < 1 || p->M > (1 << 29)) return FLTOP_ERR_BAD_SHAPE;
+    if (p->B < 1 || p->B > kMostBatch || p->N < 1 || p->M < 1 || p->M > (1 << 29)) return FLTOP_ERR_BAD_SHAPE;
     if (p->N > FLTOP_MAX_BEAM) return FLTOP_ERR_BAD_BEAM;
     const bool sigmoid = p->kind == FLTOP_PREFERENCE_SIGMOID;
     if (p->kind < FLTOP_PREFERENCE_SIGMOID || p->kind > FLTOP_PREFERENCE_SQUARE || !(p->beta > 0.0) ||
@@ -108,7 +113,7 @@ extern "C" int fltop_preference_loss(const fltop_preference* p, void* workspace,
 }
 
 extern "C" size_t fltop_policy_workspace_bytes(int32_t B, int32_t T) {
-    if (B < 1 || T < 1 || (int64_t)B * T > (int64_t)INT32_MAX) return 0;
+    if (B < 1 || B > kMostBatch || T < 1 || (int64_t)B * T > (int64_t)INT32_MAX) return 0;
     const size_t sums = fltop::policy_sums_bytes(B), rows = fltop::row_workspace_bytes(B);
     return T == 1 || sums > rows ? sums : rows;
 }
@@ -118,7 +123,7 @@ extern "C" int fltop_policy_loss(const double* scores, const double* old_scores,
                                  const fltop_policy* policy, void* workspace, size_t workspace_bytes, double* summary,
                                  double* grad_scores, void* hip_stream) {
     if (!scores || !old_scores || !advantages || !summary || !grad_scores) return FLTOP_ERR_NULL_POINTER;
-    if (B < 1 || N < 1) return FLTOP_ERR_BAD_SHAPE;
+    if (B < 1 || B > kMostBatch || N < 1) return FLTOP_ERR_BAD_SHAPE;
     int rc = check_policy(policy);
     if (rc != FLTOP_OK) return rc;
     rc = check_space(workspace, workspace_bytes, fltop_policy_workspace_bytes(B, 1));

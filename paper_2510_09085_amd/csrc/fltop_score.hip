@@ -420,8 +420,8 @@ __device__ inline double sums_by_lane(double (&v)[R]) {
 // One block of frames for one wavefront.  `in`: from the wavefront below, `out`: for the one above.  AHEAD: a table's
 // exponentials are read before all else, into registers.
 template <int K, int R, bool TABLE, bool AHEAD>
-__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t q, const double* table, bool wide, const Edge<R>& in,
-                                  Edge<R>& out, double* nowhere, const Source& from) {
+__device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t q, const double* table, bool wide,
+                                  const Edge<R>& in, Edge<R>& out, double* nowhere, const Source& from) {
     const int lane = threadIdx.x & (kWave - 1);
     const Span<R> span = {q * R, way.hi, way.reversed};
     constexpr bool kRead = TABLE && AHEAD;
@@ -1207,7 +1207,8 @@ hipError_t grad_as(const fltop_rows& x, const fltop_hypotheses& h, const double*
     const int64_t chunks = (int64_t)h.N * ((h.U + 1) / (kWave * kGradPairs - 2 * R) + 1);
     const int64_t waves = TABLE ? chunks / 6 : chunks, most = kGradThreads / kWave;
     const unsigned threads = kWave * (unsigned)(waves < 1 ? 1 : waves < most ? waves : most);
-    hipLaunchKernelGGL((score_grad_kernel<T, R, TABLE>), dim3((unsigned)(x.B * (int64_t)blocks * parts)), dim3(threads), bytes, stream, x, h, grad_scores, ws, blocks, parts, static_cast<T*>(grad));
+    hipLaunchKernelGGL((score_grad_kernel<T, R, TABLE>), dim3((unsigned)(x.B * (int64_t)blocks * parts)), dim3(threads), bytes,
+                       stream, x, h, grad_scores, ws, blocks, parts, static_cast<T*>(grad));
     return hipGetLastError();
 }
 

@@ -203,3 +203,23 @@ def test_constants_match_the_header():
     assert {"token": said["REDUCE_TOKEN"], "sequence": said["REDUCE_SEQUENCE"], "sum": said["REDUCE_SUM"]} == binding.REDUCTIONS
     assert binding.ROW_TYPES == {torch.float32: said["TYPE_F32"], torch.bfloat16: said["TYPE_BF16"],
                                  torch.float16: said["TYPE_F16"]}
+
+
+def test_more_than_a_launch_can_take(lib):
+    """Batches whose launches would have 2^32 threads or more are refused before anything is enqueued."""
+    big = 1 << 24
+    assert lib.fltop_ctc_score(ctypes.byref(rows(B=big)), ctypes.byref(hyps()), FAKE, None, 0, None) == SHAPE
+    many = ctypes.byref(rows(B=1 << 12)), ctypes.byref(hyps(N=512))
+    assert lib.fltop_ctc_score(*many, FAKE, None, 0, None) == SHAPE
+    long = ctypes.byref(rows(B=1 << 12, T=1 << 13)), ctypes.byref(hyps())
+    assert lib.fltop_ctc_score(*long, FAKE, FAKE, 1 << 62, None) == SHAPE
+    assert lib.fltop_ctc_score_grad(*long, FAKE, FAKE, 1 << 62, FAKE, None) == SHAPE
+    assert lib.fltop_ctc_score_workspace_bytes(1 << 12, 1 << 13, 3, 8) == 0
+    assert lib.fltop_ctc_score_workspace_bytes(1 << 12, 10, 512, 8) == 0
+    p = binding.FltopPreference(FAKE, None, FAKE, None, big, 4, 6, 0, 0.1, 0.1, 1.0, FAKE, FAKE, FAKE)
+    assert lib.fltop_preference_loss(ctypes.byref(p), FAKE, 1 << 62, None) == SHAPE
+    assert lib.fltop_preference_workspace_bytes(big) == 0 and lib.fltop_policy_workspace_bytes(big, 1) == 0
+    assert lib.fltop_policy_loss(FAKE, FAKE, None, FAKE, None, big, 4, ctypes.byref(settings()), FAKE, 1 << 62, FAKE, FAKE,
+                                 None) == SHAPE
+    assert lib.fltop_policy_loss_logits(ctypes.byref(rows(B=big)), FAKE, FAKE, None, FAKE, 0, ctypes.byref(settings()), FAKE,
+                                        1 << 62, FAKE, FAKE, FAKE, None) == SHAPE
