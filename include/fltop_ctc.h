@@ -423,7 +423,8 @@ int fltop_policy_loss(const double* scores, const double* old_scores, const doub
  *   summary     dev [3] fp32 as above
  *   logps       dev [B,T] fp32: l, 0 where no part is taken
  *   grad_logits dev [B,T,V] (dense, of the logits' type), 0 in frames that take no part
- * Softmax statistics are fp32, logarithms and the loss of a frame fp64.  Any V >= 1.
+ * Softmax statistics, exponentials and logarithms are fp32, log-probabilities, their
+ * differences and all sums over frames fp64.  Any V >= 1.
  * workspace: fltop_policy_workspace_bytes(B, T) bytes, 256-byte aligned. */
 int fltop_policy_loss_logits(const fltop_rows* logits, const int32_t* tokens,
                              const float* old_logps, const float* ref_logps,

@@ -630,7 +630,8 @@ def preference_loss(scores: torch.Tensor, pairs: torch.Tensor, *,
         _device_tensor(ref_scores, "ref_scores", torch.float64, (B, N), dev)
     if pair_counts is not None:
         _device_tensor(pair_counts, "pair_counts", torch.int32, (B,), dev)
-    _need(kind in PREFERENCE_KINDS, f"kind must be one of {', '.join(PREFERENCE_KINDS)}")
+    if kind not in PREFERENCE_KINDS:
+        raise ValueError(f"kind must be one of {', '.join(PREFERENCE_KINDS)}")
     with _On(scores, stream) as handle:
         grad = torch.empty_like(scores)
         loss = torch.empty((), dtype=torch.float64, device=dev)
@@ -646,7 +647,8 @@ def preference_loss(scores: torch.Tensor, pairs: torch.Tensor, *,
 
 
 def _policy(reduction, clip_low, clip_high, kl_weight, scale) -> FltopPolicy:
-    _need(reduction in REDUCTIONS, f"reduction must be one of {', '.join(REDUCTIONS)}")
+    if reduction not in REDUCTIONS:
+        raise ValueError(f"reduction must be one of {', '.join(REDUCTIONS)}")
     return FltopPolicy(REDUCTIONS[reduction], 0, clip_low, clip_high, kl_weight, scale)
 
 

@@ -88,7 +88,8 @@ struct alignas(16) Mark {
 };
 __device__ inline Kept kept(double x, int32_t e) {   // x 2^e; x is normal or 0
     const uint32_t hi = (uint32_t)((uint64_t)__double_as_longlong(x) >> 32);
-    return {0x80000000u | (uint32_t)((uint64_t)__double_as_longlong(x) >> 21), hi != 0 ? e + (int32_t)(hi >> 20) - 1022 : kNoMass};
+    const uint32_t m = 0x80000000u | (uint32_t)((uint64_t)__double_as_longlong(x) >> 21);
+    return {m, hi != 0 ? e + (int32_t)(hi >> 20) - 1022 : kNoMass};
 }
 __device__ inline Mass mass_of(Kept x) {
     const uint64_t bits = (uint64_t)(x.m & 0x7fffffffu) << 21 | 0x3fe0000000000000ull;

@@ -3,14 +3,14 @@
 // are, and there are few of them.
 //
 // A mean over what takes part needs its number before the gradient.  Small batches are one workgroup's, in one launch (64
-// pairs: 7.5 us, nearly all of it latency; two launches, as over 256 x 32 scores of a policy, take 10.5 between them).
+// pairs: 7.5 us, nearly all of it latency; 256 x 32 scores of a policy: 10.5 us in two launches, 18 by one workgroup).
 // Else one workgroup per utterance sums its own values, counts them and leaves the gradient unscaled; a second kernel adds
 // the utterances' sums up (each of its workgroups all of them, in one order) and scales.
 //
-// A hypothesis may be in many pairs: its derivatives are added in LDS as whole multiples of 2^-50 of the utterances' largest one
-// (2^-S, S less, for lists of more than 2^11 pairs), so that the order in which threads add does not matter.  A pair's derivative
-// grows with its margin for each kind of loss, so the largest one is that of the smallest or of the largest margin: a first
-// pass over the pairs makes the margins, a second one the rest.
+// A hypothesis may be in many pairs: its derivatives are added in LDS as whole multiples of 2^-50 of the workgroup's largest
+// one (of 2^-S, S less, for lists of more than 2^11 pairs), so that the order in which threads add does not matter.  A
+// pair's derivative grows with its margin for each kind of loss, so the largest one is that of the smallest or of the
+// largest margin: a first pass over the pairs makes the margins, a second one the rest.
 #include "fltop_learn.h"
 
 namespace fltop {

@@ -265,8 +265,8 @@ __device__ inline void leave_sums(const Sums& mine, double* partial) {
 }
 
 // Short rows: LANES lanes take a row, ITER vectors each, and a wavefront PASSES times kWave / LANES rows before it goes on
-// to their losses, for which each row has a lane of its own: that arithmetic, in fp64 a few hundred instructions, is done
-// once for all of them.
+// to their losses, for which each row has a lane of its own: that arithmetic, a few hundred instructions, is done once for
+// all of them.
 template <typename T, int LANES, int ITER, int PASSES>
 __global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, Frames f, fltop_policy p, T* grad) {
     constexpr int kAtOnce = kWave / LANES, kRows = kAtOnce * PASSES, N = kVec<T>;
@@ -534,7 +534,9 @@ int32_t long_rows(const fltop_rows& x, const Frames& f, const fltop_policy& p, v
 }
 
 // As few lanes as hold a row in one vector each, up to a wavefront; then as few vectors as a wavefront, a workgroup of
-// 256 and one of 1024 hold it in.
+// 256 and one of 512 hold it in; longer rows are read again.  2^25 fp32 values in rows of 32: 137 us, 385 with a wavefront for
+// each row; of 1024: 66, 107 with a workgroup; of 2048: 62 and 69; of 8192: 58, 118 if they were read again; of 32000: 65
+// and 94.  Several vectors a lane in short rows save shuffles and lose more by loads that lie apart (rows of 32: 167).
 template <typename T>
 int32_t rows_of(const fltop_rows& x, const Frames& f, const fltop_policy& p, void* grad, hipStream_t stream) {
     const int32_t vectors = (x.V + kVec<T> - 1) / kVec<T>;
@@ -545,6 +547,7 @@ int32_t rows_of(const fltop_rows& x, const Frames& f, const fltop_policy& p, voi
     if (vectors <= 64) return short_rows<T, 64, 1, 8>(x, f, p, grad, stream);
     if (vectors <= 128) return short_rows<T, 64, 2, 4>(x, f, p, grad, stream);
     if (vectors <= 256) return short_rows<T, 64, 4, 2>(x, f, p, grad, stream);
+    if (vectors <= 512) return short_rows<T, 64, 8, 1>(x, f, p, grad, stream);
     if (vectors <= 1024) return long_rows<T, 256, 4, true>(x, f, p, grad, stream);
     if (vectors <= 2048) return long_rows<T, 256, 8, true>(x, f, p, grad, stream);
     if (vectors <= 4096) return long_rows<T, 512, 8, true>(x, f, p, grad, stream);

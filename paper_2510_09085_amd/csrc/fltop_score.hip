@@ -720,7 +720,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
     const int32_t middle = middle_of<R>(y.frames);
     const Way way = {!ONE && reversed ? middle : 0, ONE || reversed ? y.frames : middle, reversed, role.side,
                      keep ? ws.marks + (at * 2 + reversed) * ws.marks_of : nullptr, (int32_t)ws.row};
-    const Way other = ONE ? way : Way{reversed ? 0 : middle, reversed ? middle : y.frames, !reversed, 1 - role.side, nullptr, 0};
+    const Way other =
+        ONE ? way : Way{reversed ? 0 : middle, reversed ? middle : y.frames, !reversed, 1 - role.side, nullptr, 0};
     if (role.tabulates) {
         if constexpr (TABLE) tabulate_all<R, kSides>(way, other, source_of(x, b), used, lds);
     } else {
