@@ -149,6 +149,7 @@ __global__ __launch_bounds__(kThreads) void part_kernel(fltop_rows x, const int3
     const int32_t b = blockIdx.x;
     const int32_t frames = min(x.lengths[b], x.T);
     int32_t n = 0;
+#pragma unroll 4
     for (int32_t t = threadIdx.x; t < frames; t += kThreads)
         n += (uint32_t)tokens[(int64_t)b * x.T + t] < (uint32_t)x.V ? 1 : 0;
 #pragma unroll
@@ -164,7 +165,7 @@ struct Frames {
     const float *old_logps, *ref_logps, *advantages;
     int32_t per_frame;
     const int32_t* counts;   // [B]
-    double* partial;         // [workgroups][3]
+    double* partial;         // [kMostRowGroups][3], and one more
     float* logps;
 };
 
@@ -249,9 +250,10 @@ __device__ inline RowGradient frame_gradient(const Frames& f, int64_t at, int32_
     return {-c / sum, c * (rest / sum)};
 }
 
-// Leaves a workgroup's sums.
+// Leaves a workgroup's sums, and the first one the number of all frames that take part.
 template <int THREADS>
-__device__ inline void leave_sums(const Sums& mine, double* partial) {
+__device__ inline void leave_sums(const Sums& mine, const Weights& weights, double* partial) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) partial[3 * kMostRowGroups] = weights.all;
     __shared__ double of_wave[THREADS / kWave][3];
     const double s[3] = {sum_of_wave(mine.loss), sum_of_wave(mine.kl), sum_of_wave(mine.clipped)};
     if (threadIdx.x % kWave == 0)
@@ -374,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 4) void short_rows_kernel(fltop_rows x, F
         }
         wave_fence();
     }
-    leave_sums<kThreads>(sums, f.partial);
+    leave_sums<kThreads>(sums, weights, f.partial);
 }
 
 // Long rows: a workgroup for each.  With HELD the row's vectors stay in registers; rows beyond what THREADS hold are read
@@ -488,16 +490,17 @@ __global__ __launch_bounds__(THREADS, 4) void long_rows_kernel(fltop_rows x, Fra
             for (int32_t c = threadIdx.x * N; c < x.V; c += THREADS * N) give(load_part(row, c, x.V), c);
         }
     }
-    leave_sums<THREADS>(sums, f.partial);
+    leave_sums<THREADS>(sums, weights, f.partial);
 }
 
-__global__ __launch_bounds__(kLongThreads) void policy_summary_kernel(const int32_t* counts, int32_t B, int32_t reduction,
-                                                                      const double* partial, int32_t groups, float* summary) {
-    __shared__ int64_t scratch[2 * kLongThreads / kWave];
+__global__ __launch_bounds__(kLongThreads) void policy_summary_kernel(const double* partial, int32_t groups, float* summary) {
     __shared__ double of_wave[kLongThreads / kWave][3];
-    const Weights weights(counts, B, reduction, scratch);
+    const double all = partial[3 * kMostRowGroups];
     Sums s;
-    for (int32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+#pragma unroll
+    for (int32_t k = 0; k < kMostRowGroups / kLongThreads; ++k) {
+        const int32_t g = k * kLongThreads + threadIdx.x;
+        if (g >= groups) continue;
         s.loss += partial[3 * g];
         s.kl += partial[3 * g + 1];
         s.clipped += partial[3 * g + 2];
@@ -509,7 +512,7 @@ __global__ __launch_bounds__(kLongThreads) void policy_summary_kernel(const int3
     if (threadIdx.x < 3) {
         double sum = 0.0;
         for (int w = 0; w < kLongThreads / kWave; ++w) sum += of_wave[w][threadIdx.x];
-        if (threadIdx.x == 2) sum = weights.all > 0.0 ? sum / weights.all : 0.0;
+        if (threadIdx.x == 2) sum = all > 0.0 ? sum / all : 0.0;
         summary[threadIdx.x] = (float)sum;
     }
 }
@@ -568,8 +571,7 @@ hipError_t launch_policy_logits(const fltop_rows& x, const int32_t* tokens, cons
     const int32_t groups = x.type == FLTOP_TYPE_BF16  ? rows_of<__hip_bfloat16>(x, f, policy, grad, stream)
                            : x.type == FLTOP_TYPE_F16 ? rows_of<__half>(x, f, policy, grad, stream)
                                                       : rows_of<float>(x, f, policy, grad, stream);
-    hipLaunchKernelGGL(policy_summary_kernel, dim3(1), dim3(kLongThreads), 0, stream, counts, x.B, policy.reduction, partial,
-                       groups, summary);
+    hipLaunchKernelGGL(policy_summary_kernel, dim3(1), dim3(kLongThreads), 0, stream, partial, groups, summary);
     return hipGetLastError();
 }
 
