@@ -29,7 +29,6 @@ struct Mass {
 constexpr int32_t kNoMass = -(1 << 30);
 
 __device__ inline Mass no_mass() { return {0.0, kNoMass}; }
-__device__ inline Mass unit_mass() { return {0.5, 1}; }
 
 // x * 2^e as a Mass.
 __device__ inline Mass normalized(double x, int32_t e) {
