@@ -157,7 +157,9 @@ __device__ inline double policy_entry(double l, double l_old, bool has_ref, doub
 inline size_t policy_sums_bytes(int32_t B) { return align_up((size_t)B * sizeof(PolicySums), 256); }
 constexpr int32_t kMostRowGroups = 2048;
 inline size_t row_counts_bytes(int32_t B) { return align_up((size_t)B * sizeof(int32_t), 256); }
-inline size_t row_workspace_bytes(int32_t B) { return row_counts_bytes(B) + (3 * kMostRowGroups + 1) * sizeof(double); }
+inline size_t row_workspace_bytes(int32_t B) {
+    return row_counts_bytes(B) + align_up((3 * kMostRowGroups + 1) * sizeof(double), 256);
+}
 
 hipError_t launch_score(const fltop_rows& x, const fltop_hypotheses& h, double* out_scores,
                         const ScoreSpace* keep, hipStream_t stream);
