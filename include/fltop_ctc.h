@@ -401,6 +401,7 @@ typedef struct fltop_policy {
     double  kl_weight;
     double  scale;                /* the gradient is that of scale * loss                         */
 } fltop_policy;
+/* Bytes for either of the two calls below, whatever T is (0 if the shapes are invalid). */
 size_t fltop_policy_workspace_bytes(int32_t B, int32_t T);
 
 /* The loss over log-probabilities that the caller has (hypotheses: fltop_ctc_score's [B,N]):

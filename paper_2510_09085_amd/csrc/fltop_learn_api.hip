@@ -114,8 +114,9 @@ extern "C" int fltop_preference_loss(const fltop_preference* p, void* workspace,
 
 extern "C" size_t fltop_policy_workspace_bytes(int32_t B, int32_t T) {
     if (B < 1 || B > kMostBatch || T < 1 || (int64_t)B * T > (int64_t)INT32_MAX) return 0;
+    // (both policy losses are asked for with T = 1: rows of hypotheses, and one token a row)
     const size_t sums = fltop::policy_sums_bytes(B), rows = fltop::row_workspace_bytes(B);
-    return T == 1 || sums > rows ? sums : rows;
+    return sums > rows ? sums : rows;
 }
 
 extern "C" int fltop_policy_loss(const double* scores, const double* old_scores, const double* ref_scores,
