@@ -495,9 +495,11 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
         z.common = false;
 #pragma unroll 1
         for (int f = 0; f < R; ++f) {
-            if (!span.real(f)) continue;
+            // (frames behind the end too: the wavefront below may have gone through them as above, and has then given
+            // up the masses of its tokens)
+            const bool real = span.real(f);
             const char* emissions = span.row(from, f);
-            const Mass blank = mass_of(value_at(emissions, 0, from.type));
+            const Mass blank = real ? mass_of(value_at(emissions, 0, from.type)) : Mass{1.0, 0};
             const Mass first = normalized(in.x[f], in.aligned ? in.e[f] : in.E);
             if (lane == kWave - 1) {
                 out.x[f] = l[K - 1].m;
@@ -512,7 +514,7 @@ __device__ inline void take_block(Lane<K, R, TABLE>& z, const Way& way, int32_t 
                 const Mass on = plus(b[k], prev);
                 const Mass p = mass_of(value_at(emissions, z.tok[k], from.type));
                 b[k] = normalized(on.m * blank.m, on.e + blank.e);
-                l[k] = z.live[k] != 0.0 ? normalized(stay.m * p.m, stay.e + p.e) : no_mass();
+                l[k] = real && z.live[k] != 0.0 ? normalized(stay.m * p.m, stay.e + p.e) : no_mass();
             }
         }
 #pragma unroll

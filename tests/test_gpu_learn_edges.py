@@ -51,3 +51,57 @@ def test_workspace_of_the_loss_over_logits(dev, B, T, V, dtype):
     assert abs(float(got["loss"]) - float(f.mean())) <= 2.0 ** -20 * float(f.abs().mean() + 1)
     with pytest.raises(binding.FltopError):
         go(workspace=ws[:-256])
+
+
+def log_lattice(lp, tokens):
+    """(ln P, occupancies [T, V]) of a hypothesis in the domain of logarithms, fp64: for masses below the 80-bit range."""
+    z = np.array(ref.states_of(tokens))
+    e = lp.astype(np.float64)[:, z]
+    S = len(z)
+    skip = np.where((np.arange(S) > 1) & (z != 0) & (z != np.roll(z, 2)), 0.0, -np.inf)
+    up = lambda x, by: np.concatenate((np.full(by, -np.inf), x[:-by]))  # noqa: E731
+    down = lambda x, by: np.concatenate((x[by:], np.full(by, -np.inf)))  # noqa: E731
+    with np.errstate(invalid="ignore"):
+        a = [np.where(np.arange(S) < 2, e[0], -np.inf)]
+        for t in range(1, len(lp)):
+            a.append(np.logaddexp(np.logaddexp(a[-1], up(a[-1], 1)), up(a[-1], 2) + skip) + e[t])
+        b = [np.where(np.arange(S) >= S - 2, 0.0, -np.inf)]
+        for t in range(len(lp) - 2, -1, -1):
+            y = b[-1] + e[t + 1]
+            b.append(np.logaddexp(np.logaddexp(y, down(y, 1)), down(y + skip, 2)))
+        total = np.logaddexp(a[-1][-1], a[-1][-2])
+        share = np.exp(np.array(a) + np.array(b[::-1]) - total)
+    out = np.zeros(lp.shape)
+    np.add.at(out.T, z, share.T)
+    return total, out
+
+
+@pytest.mark.parametrize("L,U,V,T,cost", [
+    (128, 128, 32, 257, 35), (128, 128, 32, 257, 36), (128, 128, 80, 257, 36), (128, 1100, 32, 257, 36),
+    (256, 1920, 32, 513, 64), (256, 1920, 32, 517, 64), (256, 1920, 80, 517, 63), (256, 256, 32, 515, 36)])
+def test_the_last_token_at_the_border_of_two_wavefronts(dev, L, U, V, T, cost):
+    """An utterance that ends within a block: the last token is the last of a wavefront's states, the blank behind it the
+    next one's first, and only one of them has masses close enough together for one exponent.  Every token costs e^-cost (in
+    the last block e^-38 at most), so that there is little but the one alignment, and the last token alone is likely in
+    the last two frames, where the blank is not."""
+    R = 4 if U >= 1920 else 8
+    lp = np.full((1, T, V), -float(cost), np.float32)
+    lp[0, (T - 1) // R * R:, :] = -float(min(cost, 38))
+    lp[0, :, 0] = -0.001
+    lp[0, T - 2:, V - 1] = -0.01
+    lp[0, T - 2:, 0] = -20.0
+    tok = np.zeros((1, 1, U), np.int32)
+    tok[0, 0, :L] = 1 + np.arange(L) % (V - 3)
+    tok[0, 0, L - 1] = V - 1
+    x = torch.from_numpy(lp).to(dev)
+    args = [torch.tensor(a, dtype=torch.int32, device=dev) for a in ([T], tok, [[L]])]
+    out = binding.ctc_score(x, *args, want_grad=True)
+    alone = binding.ctc_score(x, *args)["scores"]
+    grad = binding.ctc_score_grad(x, *args, torch.ones((1, 1), dtype=torch.float64, device=dev), out["workspace"])
+    want, share = log_lattice(lp[0], tok[0, 0, :L])
+    # the reference's own: each frame adds numbers of the score's size a few times, each time half a step of that off
+    slack = 4 * T * 2.0 ** -53 * abs(want)
+    for s in (out["scores"], alone):
+        assert abs(float(s) - want) <= slack + ref.score_tolerance(T, want)
+    near = ref.grad_tolerance("f32", T, share[None], share[None], np.array([2.0 * L + 1]))[0] + 4 * slack * share
+    assert np.all(np.abs(grad[0].double().cpu().numpy() - share) <= near)
