@@ -989,14 +989,19 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
     const int32_t rows = min(R, x.T - t0);
     T* const out = grad + ((int64_t)b * x.T + t0) * x.V;
     const Source from = source_of(x, b);
-    // (all of what these loads fetch is asked for before any of it is waited for)
-    const int32_t frames_raw = x.lengths[b];
+    const int32_t frames = __builtin_amdgcn_readfirstlane(min(x.lengths[b], x.T)), nf = min(R, frames - t0);
+    if (nf <= 0) {   // (nothing behind the end of an utterance is read)
+        for (int32_t f = 0; f < rows; ++f)
+            for (int32_t v = v0 + threadIdx.x; v < v1; v += blockDim.x) out[(int64_t)f * x.V + v] = from_float<T>(0.0f);
+        return;
+    }
+    // (all of what the following loads fetch is asked for before any of it is waited for)
     uint32_t block_raw[TABLE ? R : 1];
     if constexpr (TABLE) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             if (j * kWaves >= R) break;
-            const int32_t f = min(j * kWaves + wave, rows - 1), v = min(lane, x.V - 1);
+            const int32_t f = min(j * kWaves + wave, nf - 1), v = min(lane, x.V - 1);
             const char* row = from.rows + (int64_t)(t0 + f) * from.frame_bytes;
             block_raw[j] = x.type == FLTOP_TYPE_F32 ? raw_at<FLTOP_TYPE_F32>(row, v) : raw_at<FLTOP_TYPE_F16>(row, v);
         }
@@ -1011,7 +1016,6 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
         most = fmax(most, w);
     }
     for (int32_t i = threadIdx.x; i < R * width; i += blockDim.x) sums[i] = 0;
-    const int32_t frames = __builtin_amdgcn_readfirstlane(min(frames_raw, x.T)), nf = min(R, frames - t0);
     if constexpr (TABLE) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -1037,7 +1041,7 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
     }
     odd = any & 1;
     const bool wide = any & 2;
-    if (odd || most == 0.0 || nf <= 0) {
+    if (odd || most == 0.0) {
         for (int32_t f = 0; f < rows; ++f)
             for (int32_t v = v0 + threadIdx.x; v < v1; v += blockDim.x)
                 out[(int64_t)f * x.V + v] = from_float<T>(odd && f < nf ? NAN : 0.0f);

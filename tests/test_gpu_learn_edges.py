@@ -1,5 +1,6 @@
 """The operators that learn from hypotheses at the edges of their ranges: single tokens, ends of utterances at the border
 of two wavefronts, one utterance's numbers beside another's, references that are only watched."""
+import ctypes
 import math
 
 import numpy as np
@@ -105,3 +106,47 @@ def test_the_last_token_at_the_border_of_two_wavefronts(dev, L, U, V, T, cost):
         assert abs(float(s) - want) <= slack + ref.score_tolerance(T, want)
     near = ref.grad_tolerance("f32", T, share[None], share[None], np.array([2.0 * L + 1]))[0] + 4 * slack * share
     assert np.all(np.abs(grad[0].double().cpu().numpy() - share) <= near)
+
+
+@pytest.mark.parametrize("V", [32, 90])
+def test_frames_behind_the_end_are_not_read(dev, V):
+    """Room for a million frames in the call's shapes, memory for those of the utterance: same bits as without the room."""
+    frames, T, U = 43, 1 << 20, 9
+    gen = torch.Generator(device=dev).manual_seed(V)
+    x = torch.log_softmax(2 * torch.randn((1, frames, V), generator=gen, device=dev), 2)
+    lengths = torch.tensor([frames], dtype=torch.int32, device=dev)
+    tok = torch.randint(1, V, (1, 1, U), generator=gen, device=dev).to(torch.int32)
+    tl = torch.tensor([[U]], dtype=torch.int32, device=dev)
+    w = torch.ones((1, 1), dtype=torch.float64, device=dev)
+    out = binding.ctc_score(x, lengths, tok, tl, want_grad=True)
+    want = binding.ctc_score_grad(x, lengths, tok, tl, w, out["workspace"])
+
+    lib = binding.load()
+    rows = binding.FltopRows(x.data_ptr(), lengths.data_ptr(), T * V, V, 1, T, V, 0)
+    hyps = binding.FltopHypotheses(tok.data_ptr(), tl.data_ptr(), None, U, U, 1, 1, U)
+    ws = torch.empty(lib.fltop_ctc_score_workspace_bytes(1, T, 1, U), dtype=torch.uint8, device=dev)
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    for space in (None, ws):
+        score = torch.zeros((1, 1), dtype=torch.float64, device=dev)
+        assert lib.fltop_ctc_score(ctypes.byref(rows), ctypes.byref(hyps), score.data_ptr(),
+                                   None if space is None else space.data_ptr(), 0 if space is None else space.numel(),
+                                   stream) == 0
+        alone = binding.ctc_score(x, lengths, tok, tl)["scores"] if space is None else out["scores"]
+        assert torch.equal(score, alone)
+    grad = torch.full((1, T, V), 7.0, device=dev)
+    assert lib.fltop_ctc_score_grad(ctypes.byref(rows), ctypes.byref(hyps), w.data_ptr(), ws.data_ptr(), ws.numel(),
+                                    grad.data_ptr(), stream) == 0
+    assert torch.equal(grad[:, :frames], want) and not grad[:, frames:].any()
+
+    # rows of logits alike
+    per_frame = lambda v: torch.full((1, T), v, device=dev)  # noqa: E731
+    tokens = torch.randint(0, V, (1, T), generator=gen, device=dev).to(torch.int32)
+    old, A, policy = per_frame(-3.0), torch.ones(1, device=dev), binding.FltopPolicy(0, 0, 0.2, 0.2, 0.0, 1.0)
+    ws = torch.empty(lib.fltop_policy_workspace_bytes(1, T), dtype=torch.uint8, device=dev)
+    summary, logps = torch.zeros(3, device=dev), per_frame(7.0)
+    assert lib.fltop_policy_loss_logits(ctypes.byref(rows), tokens.data_ptr(), old.data_ptr(), None, A.data_ptr(), 0,
+                                        ctypes.byref(policy), ws.data_ptr(), ws.numel(), summary.data_ptr(),
+                                        logps.data_ptr(), grad.data_ptr(), stream) == 0
+    want = binding.policy_loss_logits(x, tokens[:, :frames].contiguous(), lengths, old[:, :frames].contiguous(), A)
+    assert torch.equal(grad[:, :frames], want["grad_logits"]) and not grad[:, frames:].any()
+    assert torch.equal(logps[:, :frames], want["logps"]) and not logps[:, frames:].any()
