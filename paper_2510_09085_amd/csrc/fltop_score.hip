@@ -989,7 +989,7 @@ __global__ __launch_bounds__(kGradThreads, TABLE ? 4 : 2) void score_grad_kernel
     const int32_t rows = min(R, x.T - t0);
     T* const out = grad + ((int64_t)b * x.T + t0) * x.V;
     const Source from = source_of(x, b);
-    const int32_t frames = __builtin_amdgcn_readfirstlane(min(x.lengths[b], x.T)), nf = min(R, frames - t0);
+    const int32_t frames = __builtin_amdgcn_readfirstlane(max(min(x.lengths[b], x.T), 0)), nf = min(R, frames - t0);
     if (nf <= 0) {   // (nothing behind the end of an utterance is read)
         for (int32_t f = 0; f < rows; ++f)
             for (int32_t v = v0 + threadIdx.x; v < v1; v += blockDim.x) out[(int64_t)f * x.V + v] = from_float<T>(0.0f);

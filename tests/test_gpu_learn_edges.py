@@ -150,3 +150,21 @@ def test_frames_behind_the_end_are_not_read(dev, V):
     want = binding.policy_loss_logits(x, tokens[:, :frames].contiguous(), lengths, old[:, :frames].contiguous(), A)
     assert torch.equal(grad[:, :frames], want["grad_logits"]) and not grad[:, frames:].any()
     assert torch.equal(logps[:, :frames], want["logps"]) and not logps[:, frames:].any()
+
+
+@pytest.mark.parametrize("V", [32, 90])
+def test_lengths_as_far_below_zero_as_there_are(dev, V):
+    """Clamped to no frames, in each block of the room: no gradient."""
+    B, T, U = 3, 40, 4
+    x = torch.log_softmax(torch.randn((B, T, V), generator=torch.Generator(device=dev).manual_seed(V), device=dev), 2)
+    lengths = torch.tensor([-2 ** 31, -2 ** 31 + 1, 40], dtype=torch.int32, device=dev)
+    tok = torch.ones((B, 2, U), dtype=torch.int32, device=dev)
+    tl = torch.tensor([[0, 2]] * B, dtype=torch.int32, device=dev)
+    ws = torch.zeros(binding.score_workspace_bytes(B, T, 2, U), dtype=torch.uint8, device=dev)
+    out = binding.ctc_score(x, lengths, tok, tl, want_grad=True, workspace=ws)
+    grad = binding.ctc_score_grad(x, lengths, tok, tl, torch.ones((B, 2), dtype=torch.float64, device=dev), ws)
+    assert out["scores"][:2].tolist() == [[0.0, -math.inf]] * 2 and torch.isfinite(out["scores"][2]).all()
+    assert not grad[:2].any() and grad[2].any()
+    old = torch.zeros((B, T), device=dev)
+    told = binding.policy_loss_logits(x, torch.ones((B, T), dtype=torch.int32, device=dev), lengths, old, old[:, 0].contiguous() + 1)
+    assert not told["grad_logits"][:2].any() and not told["logps"][:2].any() and told["grad_logits"][2].any()
