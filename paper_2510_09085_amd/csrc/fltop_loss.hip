@@ -344,8 +344,8 @@ hipError_t launch_preference(const fltop_preference& p, void* workspace, hipStre
         return hipGetLastError();
     }
     // 128 utterances of 4950 pairs: 29 us with 256 threads, 20 us with 1024, about half of which are the exponentials and
-    // logarithms of the 128 compute units in use.
-    if (p.M > kThreads * 2)
+    // logarithms of the 128 compute units in use.  (A launch has fewer than 2^32 threads.)
+    if (p.M > kThreads * 2 && (int64_t)p.B * kOneThreads < (int64_t)1 << 32)
         hipLaunchKernelGGL((preference_kernel<kOneThreads, false>), dim3(p.B), dim3(kOneThreads), (size_t)p.N * 16, stream, p,
                            sums);
     else

@@ -168,3 +168,22 @@ def test_lengths_as_far_below_zero_as_there_are(dev, V):
     old = torch.zeros((B, T), device=dev)
     told = binding.policy_loss_logits(x, torch.ones((B, T), dtype=torch.int32, device=dev), lengths, old, old[:, 0].contiguous() + 1)
     assert not told["grad_logits"][:2].any() and not told["logps"][:2].any() and told["grad_logits"][2].any()
+
+
+def test_lists_of_pairs_of_as_many_utterances_as_a_launch_takes(dev):
+    """2^22 utterances, of more pairs than a small workgroup is taken for: the same number everywhere."""
+    B, M = 1 << 22, 513
+    pairs = torch.zeros((B, M, 2), dtype=torch.int32, device=dev)
+    pairs[:, :, 1] = 1
+    scores = torch.tensor([[3.0, 1.0]], dtype=torch.float64, device=dev).expand(B, 2).contiguous()
+    out = binding.preference_loss(scores, pairs, beta=0.5, scale=float(B))
+    del pairs
+    assert bool((out["margins"] == 2.0).all())
+    del out["margins"]
+    # each loss ln(1 + 1/e); sums of M and of B terms, half a step each at most
+    assert abs(float(out["loss"]) - math.log1p(math.exp(-1.0))) <= (B + M) * 2.0 ** -53
+    want = -0.5 / (1.0 + math.e)
+    got = out["grad_scores"]
+    assert torch.equal(got, got[:1].expand_as(got))
+    assert abs(float(got[0, 0]) - want) <= M * 2.0 ** -52 and float(got[0, 1]) == -float(got[0, 0])
+    torch.cuda.empty_cache()
