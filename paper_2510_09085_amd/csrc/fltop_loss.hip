@@ -350,6 +350,8 @@ hipError_t launch_preference(const fltop_preference& p, void* workspace, hipStre
                            sums);
     else
         hipLaunchKernelGGL((preference_kernel<kThreads, false>), dim3(p.B), dim3(kThreads), (size_t)p.N * 16, stream, p, sums);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(preference_mean_kernel, dim3(blocks_for(scores)), dim3(kThreads), 0, stream, p, sums);
     return hipGetLastError();
 }
@@ -366,6 +368,8 @@ hipError_t launch_policy(const double* scores, const double* old_scores, const d
     }
     hipLaunchKernelGGL(policy_kernel, dim3(B), dim3(kThreads), 0, stream, scores, old_scores, ref_scores, advantages,
                        counts, N, policy, sums, grad_scores);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(policy_mean_kernel, dim3(blocks_for((int64_t)B * N)), dim3(kThreads), 0, stream, sums, B, N,
                        policy, summary, grad_scores);
     return hipGetLastError();

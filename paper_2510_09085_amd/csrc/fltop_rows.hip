@@ -567,10 +567,14 @@ hipError_t launch_policy_logits(const fltop_rows& x, const int32_t* tokens, cons
     int32_t* const counts = static_cast<int32_t*>(workspace);
     double* const partial = reinterpret_cast<double*>(static_cast<char*>(workspace) + row_counts_bytes(x.B));
     hipLaunchKernelGGL(part_kernel, dim3(x.B), dim3(kThreads), 0, stream, x, tokens, counts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     const Frames f = {tokens, old_logps, ref_logps, advantages, per_frame, counts, partial, logps};
     const int32_t groups = x.type == FLTOP_TYPE_BF16  ? rows_of<__hip_bfloat16>(x, f, policy, grad, stream)
                            : x.type == FLTOP_TYPE_F16 ? rows_of<__half>(x, f, policy, grad, stream)
                                                       : rows_of<float>(x, f, policy, grad, stream);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(policy_summary_kernel, dim3(1), dim3(kLongThreads), 0, stream, partial, groups, summary);
     return hipGetLastError();
 }
