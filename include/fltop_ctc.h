@@ -389,7 +389,9 @@ int fltop_preference_loss(const fltop_preference* p, void* workspace, size_t wor
  *     kl = exp(l_ref - l) - (l_ref - l) - 1                    (0 without a reference)
  * reduced over everything that takes part: FLTOP_REDUCE_TOKEN the mean of all, _SEQUENCE the
  * mean over the rows b (that have any) of each row's mean, _SUM the sum.  The gradient goes
- * through r where A r is not above its clipped value.  Nothing takes part: 0. */
+ * through r where A r is not above its clipped value.  With a kl_weight of 0 the reference is
+ * only watched: kl is reported, loss and gradient do not see it, infinite or not.  Nothing takes
+ * part: 0. */
 #define FLTOP_REDUCE_TOKEN    0
 #define FLTOP_REDUCE_SEQUENCE 1
 #define FLTOP_REDUCE_SUM      2
@@ -424,6 +426,9 @@ int fltop_policy_loss(const double* scores, const double* old_scores, const doub
  *   summary     dev [3] fp32 as above
  *   logps       dev [B,T] fp32: l, 0 where no part is taken
  *   grad_logits dev [B,T,V] (dense, of the logits' type), 0 in frames that take no part
+ * A logit of -inf is a mask.  A token without mass has l = -inf: its ratio is 0, its kl +inf.  Other
+ * numbers of frames that take part have to be finite: what is not, and rows without a finite
+ * logit, give what the formulas give.
  * Softmax statistics, exponentials and logarithms are fp32, log-probabilities, their
  * differences and all sums over frames fp64.  Any V >= 1.
  * workspace: fltop_policy_workspace_bytes(B, T) bytes, 256-byte aligned. */

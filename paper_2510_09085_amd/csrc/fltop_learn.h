@@ -143,12 +143,14 @@ __device__ inline double policy_entry(double l, double l_old, bool has_ref, doub
     const double cut = fmin(fmax(r, 1.0 - p.clip_low), 1.0 + p.clip_high) * A;
     const double gap = has_ref ? l_ref - l : 0.0;
     const double e = expm1(gap);
-    const double kl = e - gap;
-    s->loss += fmax(-plain, -cut) + p.kl_weight * kl;
+    const double kl = e < INFINITY ? e - gap : e;
+    // (a weight of 0 leaves the KL out: it may be infinite)
+    const bool weighs = p.kl_weight != 0.0;
+    s->loss += fmax(-plain, -cut) + (weighs ? p.kl_weight * kl : 0.0);
     s->kl += kl;
     s->clipped += plain > cut ? 1.0 : 0.0;
     s->n += 1.0;
-    return (plain <= cut ? -plain : 0.0) - p.kl_weight * e;
+    return (plain <= cut ? -plain : 0.0) - (weighs ? p.kl_weight * e : 0.0);
 }
 
 

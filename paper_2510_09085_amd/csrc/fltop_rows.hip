@@ -214,9 +214,17 @@ struct RowGradient {
     float by, own;
 };
 
-// exp(x) - x - 1 with its digits where x is small: x^2 (1/2 + x/6 + .. + x^6/40320) leaves out x^9/9!, below 2^-27 of it.
-__device__ inline float exp_beyond_line(float x) {
-    if (fabsf(x) > 0.5f) return expm1f(x) - x;
+// exp(x) - x - 1 and exp(x) - 1, with their digits where x is small: x^2 (1/2 + x/6 + .. + x^6/40320) leaves out
+// x^9/9!, below 2^-24 of it.  Infinities are what the formulas give.
+struct Beyond {
+    float kl;
+    double slope;
+};
+__device__ inline Beyond exp_beyond_line(float x) {
+    if (fabsf(x) > 0.5f) {
+        const float e = expm1f(x);
+        return {e < INFINITY ? e - x : e, e};
+    }
     float p = 1.0f / 40320.0f;
     p = fmaf(p, x, 1.0f / 5040.0f);
     p = fmaf(p, x, 1.0f / 720.0f);
@@ -224,7 +232,8 @@ __device__ inline float exp_beyond_line(float x) {
     p = fmaf(p, x, 1.0f / 24.0f);
     p = fmaf(p, x, 1.0f / 6.0f);
     p = fmaf(p, x, 0.5f);
-    return p * x * x;
+    const float kl = p * x * x;
+    return {kl, (double)kl + x};
 }
 
 // A frame of a token, from its row's statistics: rest = sum of exp(x_v - top) over v other than the token (so that 1 - p
@@ -240,10 +249,12 @@ __device__ inline RowGradient frame_gradient(const Frames& f, int64_t at, int32_
     const float cut_r = fminf(fmaxf(r, (float)(1.0 - p.clip_low)), (float)(1.0 + p.clip_high));
     const float plain = r * A, cut = cut_r * A;
     const float beyond = f.ref_logps ? (float)(f.ref_logps[at] - l) : 0.0f;
-    const float kl = exp_beyond_line(beyond);
-    const double d = (plain <= cut ? -(double)plain : 0.0) - p.kl_weight * ((double)kl + beyond);
-    sums->loss += (fmaxf(-plain, -cut) + p.kl_weight * kl) * weight;
-    sums->kl += kl * weight;
+    const Beyond kl = exp_beyond_line(beyond);
+    // (a weight of 0 leaves the KL out: it may be infinite)
+    const bool weighs = p.kl_weight != 0.0;
+    const double d = (plain <= cut ? -(double)plain : 0.0) - (weighs ? p.kl_weight * kl.slope : 0.0);
+    sums->loss += (fmaxf(-plain, -cut) + (weighs ? p.kl_weight * kl.kl : 0.0)) * weight;
+    sums->kl += kl.kl * weight;
     sums->clipped += plain > cut ? 1.0 : 0.0;
     f.logps[at] = (float)l;
     const float c = (float)(d * (weight * p.scale));

@@ -187,3 +187,59 @@ def test_lists_of_pairs_of_as_many_utterances_as_a_launch_takes(dev):
     assert torch.equal(got, got[:1].expand_as(got))
     assert abs(float(got[0, 0]) - want) <= M * 2.0 ** -52 and float(got[0, 1]) == -float(got[0, 0])
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("V", [30, 9000])
+def test_a_reference_over_logits_that_is_only_watched(dev, V):
+    """kl_weight 0: a KL that overflows, and that of a token without mass, touch neither loss nor gradient."""
+    gen = torch.Generator(device=dev).manual_seed(V)
+    x = torch.randn((2, 3, V), generator=gen, device=dev)
+    tok = torch.full((2, 3), 5, dtype=torch.int32, device=dev)
+    x[1, 1, 5] = -math.inf
+    lengths = torch.full((2,), 3, dtype=torch.int32, device=dev)
+    old = torch.full((2, 3), -math.log(V), device=dev)
+    A = torch.tensor([1.0, -0.5], device=dev)
+    far = old.clone()
+    far[0, 1] += 100.0
+    go = lambda q, w: binding.policy_loss_logits(x, tok, lengths, old, A, ref_logps=q, kl_weight=w)  # noqa: E731
+    alone = go(None, 0.0)
+    assert math.isfinite(float(alone["loss"])) and float(alone["kl"]) == 0.0
+    for q in (far, old):
+        seen = go(q, 0.0)
+        for k in ("loss", "clipped", "logps", "grad_logits"):
+            assert torch.equal(seen[k], alone[k]), k
+        assert float(seen["kl"]) == math.inf
+    # with a weight they are what the formulas give
+    assert float(go(far, 0.1)["loss"]) == math.inf
+    # a reference that rules a token out: infinite KL, of slope 1
+    x[1, 1, 5] = 0.0
+    far[:] = old
+    far[0, 0] = -math.inf
+    ruled, near = go(far, 0.25), go(old, 0.25)
+    assert float(ruled["loss"]) == math.inf and float(ruled["kl"]) == math.inf
+    l = ruled["logps"][0, 0].double()
+    # d/dl: 1 in place of 1 - exp(ref - l), of six frames, at the token times 1 - p
+    want = 0.25 / 6 * math.exp(float(old[0, 0]) - float(l)) * (1 - math.exp(float(l)))
+    got = float(ruled["grad_logits"][0, 0, 5].double() - near["grad_logits"][0, 0, 5].double())
+    # both derivatives below 4 and their parts rounded to fp32 some 20 times
+    assert abs(got - want) <= 4 * 20 * 2.0 ** -24
+    assert torch.equal(ruled["grad_logits"][:, 1:], near["grad_logits"][:, 1:])
+
+
+@pytest.mark.parametrize("B,N", [(2, 3), (40, 64)])
+def test_a_reference_of_scores_that_is_only_watched(dev, B, N):
+    """The same over scores, in one launch and in two: a gap of 800, and one that no double holds."""
+    s = -20 * torch.rand((B, N), dtype=torch.float64, generator=torch.Generator(device=dev).manual_seed(N), device=dev)
+    A = torch.ones_like(s)
+    go = lambda q, w: binding.policy_loss(s, s + 0.1, A, ref_scores=q, kl_weight=w)  # noqa: E731
+    alone = go(None, 0.0)
+    for gap in (800.0, 1.7e308):
+        q = s.clone()
+        q[1, 2] += gap
+        seen = go(q, 0.0)
+        for k in ("loss", "clipped", "grad_scores"):
+            assert torch.equal(seen[k], alone[k]), k
+        assert float(seen["kl"]) == math.inf and float(go(q, 0.1)["loss"]) == math.inf
+    s[1, 2], q[1, 2] = -1.7e308, 1.7e308
+    assert float(binding.policy_loss(s, s, A, ref_scores=q)["kl"]) == math.inf
+    assert math.isfinite(float(binding.policy_loss(s, s, A, ref_scores=q)["loss"]))
