@@ -3,14 +3,15 @@
 // are, and there are few of them.
 //
 // A mean over what takes part needs its number before the gradient.  Small batches are one workgroup's, in one launch (64
-// pairs: 7.5 us, nearly all of it latency; 256 x 32 scores of a policy: 10.5 us in two launches, 18 by one workgroup).
+// pairs: 4.6 us, nearly all of it latency; 256 x 32 scores of a policy: 10.5 us in two launches, 18 by one workgroup).
 // Else one workgroup per utterance sums its own values, counts them and leaves the gradient unscaled; a second kernel adds
 // the utterances' sums up (each of its workgroups all of them, in one order) and scales.
 //
-// A hypothesis may be in many pairs: its derivatives are added in LDS as whole multiples of 2^-50 of the workgroup's largest
-// one (of 2^-S, S less, for lists of more than 2^11 pairs), so that the order in which threads add does not matter.  A
-// pair's derivative grows with its margin for each kind of loss, so the largest one is that of the smallest or of the
-// largest margin: a first pass over the pairs makes the margins, a second one the rest.
+// A hypothesis may be in many pairs: its derivatives are added in LDS as whole multiples of 2^-50 of its utterance's largest
+// one (of 2^-S, S less, for lists of more than 2^11 pairs), so that the order in which threads add does not matter.  The
+// one workgroup of a small batch keeps its pairs' derivatives in registers while the largest are found, each utterance's
+// for itself.  Longer lists: a pair's derivative grows with its margin for each kind of loss, so the largest one is that
+// of the smallest or of the largest margin, a first pass over the pairs makes the margins, a second one the rest.
 #include "fltop_learn.h"
 
 namespace fltop {
@@ -103,38 +104,96 @@ __device__ inline int32_t pairs_of(const fltop_preference& p, int32_t b) {
     return count < 0 ? 0 : (count > p.M ? p.M : count);
 }
 
-// One workgroup's utterances: all of them with ONE, else its own.  LDS holds their log ratios and their derivatives' sums.
-template <int THREADS, bool ONE>
+__device__ inline int2 pair_at(const int32_t* list, int64_t m) {
+    int2 pair;
+    __builtin_memcpy(&pair, list + 2 * m, sizeof(pair));
+    return pair;
+}
+
+// A pair's margin from the log ratios of its utterance, NaN if it takes no part.
+__device__ inline double margin_of(const fltop_preference& p, const double* ratio, int2 pair, bool there) {
+    const bool fine = there && (uint32_t)pair.x < (uint32_t)p.N && (uint32_t)pair.y < (uint32_t)p.N;
+    const double h = fine ? ratio[pair.x] - ratio[pair.y] : NAN;
+    return isfinite(h) ? h : NAN;
+}
+
+// A small batch in one workgroup.  LDS holds the log ratios, their derivatives' sums, and each utterance's largest
+// derivative (as bits: those of numbers from 0 up are ordered as they are).
+__global__ __launch_bounds__(kOneThreads) void preference_one_kernel(fltop_preference p) {
+    extern __shared__ double shared[];
+    __shared__ double scratch[kOneThreads / kWave];
+    constexpr int kEach = kOnePairs / kOneThreads;
+    const int32_t count = p.B * p.N, pairs = p.B * p.M;
+    double* const ratio = shared;
+    unsigned long long* const slopes = reinterpret_cast<unsigned long long*>(shared + count);
+    unsigned long long* const most = slopes + count;
+    int2 pair[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int32_t m = k * kOneThreads + threadIdx.x;
+        pair[k] = m < pairs ? pair_at(p.pairs, m) : int2{0, 0};
+    }
+    for (int32_t i = threadIdx.x; i < count; i += kOneThreads) {
+        ratio[i] = log_ratio(p, i);
+        slopes[i] = 0;
+    }
+    for (int32_t b = threadIdx.x; b < p.B; b += kOneThreads) most[b] = 0;
+    __syncthreads();
+    double loss = 0.0, used = 0.0, slope[kEach];
+    int32_t of[kEach];   // the pair's utterance, -1 if it takes no part
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int32_t m = k * kOneThreads + threadIdx.x, b = (uint32_t)m / (uint32_t)p.M;
+        of[k] = -1;
+        if (m >= pairs) continue;
+        const double h = margin_of(p, ratio + b * p.N, pair[k], m - b * p.M < pairs_of(p, b));
+        p.margins[m] = h;
+        double f;
+        if (!pair_loss(p, h, &f, &slope[k])) continue;
+        loss += f;
+        used += 1.0;
+        of[k] = b;
+        atomicMax(&most[b], (unsigned long long)__double_as_longlong(fabs(slope[k])));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        const int32_t b = of[k];
+        if (b < 0) continue;
+        const unsigned long long whole = Steps(__longlong_as_double((long long)most[b]), p.M).whole(slope[k]);
+        atomicAdd(&slopes[b * p.N + pair[k].x], whole);
+        atomicAdd(&slopes[b * p.N + pair[k].y], 0ull - whole);
+    }
+    loss = block_sum(loss, scratch);
+    used = block_sum(used, scratch);
+    const double by = used > 0.0 ? p.scale / used : 0.0;
+    if (threadIdx.x == 0) *p.loss = used > 0.0 ? loss / used : 0.0;
+    for (int32_t i = threadIdx.x; i < count; i += kOneThreads) {
+        const Steps steps(__longlong_as_double((long long)most[(uint32_t)i / (uint32_t)p.N]), p.M);
+        p.grad_scores[i] = steps.value(slopes[i]) * by;
+    }
+}
+
+// A workgroup for each utterance.  LDS holds its log ratios and their derivatives' sums.
+template <int THREADS>
 __global__ __launch_bounds__(THREADS) void preference_kernel(fltop_preference p, PairSums* sums) {
     extern __shared__ double shared[];
     __shared__ double scratch[THREADS / kWave];
-    const int32_t b0 = ONE ? 0 : blockIdx.x, count = (ONE ? p.B : 1) * p.N;
-    const int64_t pairs = (int64_t)(ONE ? p.B : 1) * p.M;
+    const int32_t b = blockIdx.x;
     double* const ratio = shared;
-    unsigned long long* const slopes = reinterpret_cast<unsigned long long*>(shared + count);
-    for (int32_t i = threadIdx.x; i < count; i += THREADS) {
-        ratio[i] = log_ratio(p, (int64_t)b0 * p.N + i);
+    unsigned long long* const slopes = reinterpret_cast<unsigned long long*>(shared + p.N);
+    for (int32_t i = threadIdx.x; i < p.N; i += THREADS) {
+        ratio[i] = log_ratio(p, (int64_t)b * p.N + i);
         slopes[i] = 0;
     }
     __syncthreads();
-    const int32_t* const list = p.pairs + (int64_t)b0 * p.M * 2;
-    double* const margins = p.margins + (int64_t)b0 * p.M;
-    auto pair_at = [&](int64_t m) {
-        int2 pair;
-        __builtin_memcpy(&pair, list + 2 * m, sizeof(pair));
-        return pair;
-    };
-    auto first_of = [&](int64_t m) { return ONE ? (int32_t)((uint32_t)m / (uint32_t)p.M) : 0; };
+    const int32_t* const list = p.pairs + (int64_t)b * p.M * 2;
+    double* const margins = p.margins + (int64_t)b * p.M;
+    const int32_t there = pairs_of(p, b);
     double high = -INFINITY, low = INFINITY;
 #pragma unroll 4
-    for (int64_t m = threadIdx.x; m < pairs; m += THREADS) {
-        const int32_t b = first_of(m);
-        const int2 pair = pair_at(m);
-        double h = NAN;
-        if ((int32_t)(m - (int64_t)b * p.M) < pairs_of(p, b0 + b) && (uint32_t)pair.x < (uint32_t)p.N &&
-            (uint32_t)pair.y < (uint32_t)p.N)
-            h = ratio[b * p.N + pair.x] - ratio[b * p.N + pair.y];
-        if (!isfinite(h)) h = NAN;
+    for (int32_t m = threadIdx.x; m < p.M; m += THREADS) {
+        const double h = margin_of(p, ratio, pair_at(list, m), m < there);
         margins[m] = h;
         high = fmax(high, h);   // (NaN is passed over)
         low = fmin(low, h);
@@ -144,29 +203,21 @@ __global__ __launch_bounds__(THREADS) void preference_kernel(fltop_preference p,
     const Steps steps(fmax(slope_of(p, high), slope_of(p, low)), p.M);
     double loss = 0.0, used = 0.0;
 #pragma unroll 4
-    for (int64_t m = threadIdx.x; m < pairs; m += THREADS) {
+    for (int32_t m = threadIdx.x; m < p.M; m += THREADS) {
         const double h = margins[m];
-        const int2 pair = pair_at(m);
+        const int2 pair = pair_at(list, m);
         double f, g;
         if (!pair_loss(p, h, &f, &g)) continue;
         loss += f;
         used += 1.0;
         const unsigned long long whole = steps.whole(g);
-        const int32_t b = first_of(m);
-        atomicAdd(&slopes[b * p.N + pair.x], whole);
-        atomicAdd(&slopes[b * p.N + pair.y], 0ull - whole);
+        atomicAdd(&slopes[pair.x], whole);
+        atomicAdd(&slopes[pair.y], 0ull - whole);
     }
     loss = block_sum(loss, scratch);
     used = block_sum(used, scratch);
-    const double by = ONE ? (used > 0.0 ? p.scale / used : 0.0) : 1.0;
-    if (threadIdx.x == 0) {
-        if constexpr (ONE)
-            *p.loss = used > 0.0 ? loss / used : 0.0;
-        else
-            sums[b0] = {loss, used};
-    }
-    for (int32_t i = threadIdx.x; i < count; i += THREADS)
-        p.grad_scores[(int64_t)b0 * p.N + i] = steps.value(slopes[i]) * by;
+    if (threadIdx.x == 0) sums[b] = {loss, used};
+    for (int32_t i = threadIdx.x; i < p.N; i += THREADS) p.grad_scores[(int64_t)b * p.N + i] = steps.value(slopes[i]);
 }
 
 __global__ __launch_bounds__(kThreads) void preference_mean_kernel(fltop_preference p, const PairSums* sums) {
@@ -339,17 +390,16 @@ hipError_t launch_preference(const fltop_preference& p, void* workspace, hipStre
     PairSums* sums = static_cast<PairSums*>(workspace);
     const int64_t scores = (int64_t)p.B * p.N, pairs = (int64_t)p.B * p.M;
     if (scores <= kOneScores && pairs <= kOnePairs) {
-        hipLaunchKernelGGL((preference_kernel<kOneThreads, true>), dim3(1), dim3(kOneThreads), (size_t)scores * 16, stream, p,
-                           sums);
+        hipLaunchKernelGGL(preference_one_kernel, dim3(1), dim3(kOneThreads), (size_t)scores * 16 + (size_t)p.B * 8, stream, p);
         return hipGetLastError();
     }
     // 128 utterances of 4950 pairs: 29 us with 256 threads, 20 us with 1024, about half of which are the exponentials and
     // logarithms of the 128 compute units in use.  (A launch has fewer than 2^32 threads.)
     if (p.M > kThreads * 2 && (int64_t)p.B * kOneThreads < (int64_t)1 << 32)
-        hipLaunchKernelGGL((preference_kernel<kOneThreads, false>), dim3(p.B), dim3(kOneThreads), (size_t)p.N * 16, stream, p,
+        hipLaunchKernelGGL((preference_kernel<kOneThreads>), dim3(p.B), dim3(kOneThreads), (size_t)p.N * 16, stream, p,
                            sums);
     else
-        hipLaunchKernelGGL((preference_kernel<kThreads, false>), dim3(p.B), dim3(kThreads), (size_t)p.N * 16, stream, p, sums);
+        hipLaunchKernelGGL((preference_kernel<kThreads>), dim3(p.B), dim3(kThreads), (size_t)p.N * 16, stream, p, sums);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(preference_mean_kernel, dim3(blocks_for(scores)), dim3(kThreads), 0, stream, p, sums);

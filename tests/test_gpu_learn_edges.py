@@ -243,3 +243,23 @@ def test_a_reference_of_scores_that_is_only_watched(dev, B, N):
     s[1, 2], q[1, 2] = -1.7e308, 1.7e308
     assert float(binding.policy_loss(s, s, A, ref_scores=q)["kl"]) == math.inf
     assert math.isfinite(float(binding.policy_loss(s, s, A, ref_scores=q)["loss"]))
+
+
+@pytest.mark.parametrize("B", [2, 64, 2000])
+@pytest.mark.parametrize("kind", ["sigmoid", "square"])
+def test_one_utterance_does_not_set_the_digits_of_another(dev, kind, B):
+    """A derivative of 1e17, or ones of e^-40, beside those of other utterances: each keeps 50 bits of its own, in a batch of
+    one launch (up to 2048 scores) as in a larger one."""
+    rng = np.random.default_rng(B)
+    s = -20 * rng.random((B, 2))
+    s[0] = (1e17, 0.0) if kind == "square" else (-20.0, 0.0)
+    s[1:, 0] += 0.0 if kind == "square" else 450.0
+    pairs = np.tile(np.array([[[0, 1]]], np.int32), (B, 1, 1))
+    S, P = torch.from_numpy(s).to(dev), torch.from_numpy(pairs).to(dev)
+    got = binding.preference_loss(S, P, kind=kind, beta=0.1)["grad_scores"].cpu().numpy()
+    h = s[:, 0] - s[:, 1]
+    want = (2 * (h - 5.0) if kind == "square" else -0.1 / (1.0 + np.exp(0.1 * h))) / B
+    # the margin's difference, beta's product with it (45 * 2^-53 in e^x) and some ten roundings; a step of 2^-50
+    tol = (45 + 20) * 2.0 ** -53 + 2.0 ** -50
+    scale = np.abs(want) + (2 * 2.0 ** -53 * (np.abs(s).sum(1) + 5.0) / B / tol if kind == "square" else 0.0)
+    assert np.all(np.abs(got[:, 0] - want) <= tol * scale) and np.array_equal(got[:, 1], -got[:, 0])
