@@ -361,8 +361,8 @@ int fltop_ctc_score_grad(const fltop_rows* logprobs, const fltop_hypotheses* hyp
  * The result is the mean over the pairs that take part: those before pair_counts[b] whose two
  * indices are in [0,N), whose scores are all finite and whose margin is.  A pair may appear
  * twice (it counts twice) and hypotheses may be shared by pairs (their gradients add up, as whole
- * multiples of 2^-50 of the utterance's largest derivative; of 2^-(61 - k) for lists of 2^k pairs
- * where that is more).  No pair that takes part: loss 0. */
+ * multiples of 2^-50 of the utterance's largest derivative; of 2^-(60 - k) for lists of 2^k pairs
+ * and more where that is more).  No pair that takes part: loss 0. */
 #define FLTOP_PREFERENCE_SIGMOID 0
 #define FLTOP_PREFERENCE_HINGE   1
 #define FLTOP_PREFERENCE_SQUARE  2

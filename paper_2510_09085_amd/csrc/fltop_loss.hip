@@ -8,7 +8,7 @@
 // the utterances' sums up (each of its workgroups all of them, in one order) and scales.
 //
 // A hypothesis may be in many pairs: its derivatives are added in LDS as whole multiples of 2^-50 of its utterance's largest
-// one (of 2^-S, S less, for lists of more than 2^11 pairs), so that the order in which threads add does not matter.  The
+// one (of 2^-S, S less, for lists of 2^11 pairs and more), so that the order in which threads add does not matter.  The
 // one workgroup of a small batch keeps its pairs' derivatives in registers while the largest are found, each utterance's
 // for itself.  Longer lists: a pair's derivative grows with its margin for each kind of loss, so the largest one is that
 // of the smallest or of the largest margin, a first pass over the pairs makes the margins, a second one the rest.
@@ -57,7 +57,8 @@ __device__ inline bool pair_loss(const fltop_preference& p, double h, double* lo
     if (p.kind == FLTOP_PREFERENCE_SIGMOID) {
         const double e = exp(-fabs(x)), l = log1p(e);
         // ln(1 + e^-x) and ln(1 + e^x), sigma(x)
-        *loss = (1.0 - p.label_smoothing) * (fmax(-x, 0.0) + l) + p.label_smoothing * (fmax(x, 0.0) + l);
+        *loss = (1.0 - p.label_smoothing) * (fmax(-x, 0.0) + l);
+        if (p.label_smoothing > 0.0) *loss += p.label_smoothing * (fmax(x, 0.0) + l);   // (x may be infinite)
         // sigma(x) - (1 - label_smoothing), without cancellation where nothing is smoothed
         *slope = p.beta * (p.label_smoothing - (x >= 0.0 ? e : 1.0) / (1.0 + e));
     } else if (p.kind == FLTOP_PREFERENCE_HINGE) {

@@ -263,3 +263,17 @@ def test_one_utterance_does_not_set_the_digits_of_another(dev, kind, B):
     tol = (45 + 20) * 2.0 ** -53 + 2.0 ** -50
     scale = np.abs(want) + (2 * 2.0 ** -53 * (np.abs(s).sum(1) + 5.0) / B / tol if kind == "square" else 0.0)
     assert np.all(np.abs(got[:, 0] - want) <= tol * scale) and np.array_equal(got[:, 1], -got[:, 0])
+
+
+@pytest.mark.parametrize("B", [1, 3000])
+def test_a_margin_that_beta_takes_out_of_range(dev, B):
+    """Won by more than a double holds: no loss and no gradient; lost by as much: an infinite loss of slope -beta."""
+    s = torch.tensor([[1e300, -1e300]], dtype=torch.float64, device=dev).repeat(B, 1)
+    won = torch.tensor([[[0, 1]]], dtype=torch.int32, device=dev).repeat(B, 1, 1)
+    out = binding.preference_loss(s, won, beta=1e10)
+    assert float(out["loss"]) == 0.0 and not out["grad_scores"].any()
+    out = binding.preference_loss(s, won.flip(2).contiguous(), beta=1e10, scale=float(B))
+    assert float(out["loss"]) == math.inf and out["grad_scores"][-1].tolist() == [1e10, -1e10]
+    for smoothed in (won, won.flip(2).contiguous()):
+        out = binding.preference_loss(s, smoothed, beta=1e10, label_smoothing=0.25)
+        assert float(out["loss"]) == math.inf and torch.isfinite(out["grad_scores"]).all()
