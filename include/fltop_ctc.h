@@ -332,8 +332,8 @@ typedef struct fltop_hypotheses {
  *              fltop_ctc_score_workspace_bytes(B, T, N, U) bytes, into which the call puts what
  *              fltop_ctc_score_grad goes on from.
  * Refused: B, T, N < 1, V < 2, U < 1 or beyond FLTOP_MAX_LABELS, B >= 2^24, B * N >= 2^21 or
- * B * T >= 2^31, with a workspace B * (T / 8 + 1) >= 2^22 too (BAD_SHAPE), N > FLTOP_MAX_BEAM (BAD_BEAM), V > FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type
- * (BAD_OPTION). */
+ * B * T >= 2^31 - 2^13, with a workspace B * (T / 8 + 1) >= 2^22 too (BAD_SHAPE), N > FLTOP_MAX_BEAM
+ * (BAD_BEAM), V > FLTOP_MAX_VOCAB (VOCAB_TOO_BIG), an unknown type (BAD_OPTION). */
 size_t fltop_ctc_score_workspace_bytes(int32_t B, int32_t T, int32_t N, int32_t U);
 int fltop_ctc_score(const fltop_rows* logprobs, const fltop_hypotheses* hyps, double* out_scores,
                     void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -408,7 +408,7 @@ typedef struct fltop_policy {
 size_t fltop_policy_workspace_bytes(int32_t B, int32_t T);
 
 /* The loss over log-probabilities that the caller has (hypotheses: fltop_ctc_score's [B,N]):
- *   scores, old_scores, ref_scores (or NULL), advantages   dev [B,N], B < 2^24
+ *   scores, old_scores, ref_scores (or NULL), advantages   dev [B,N], B < 2^24, N < 2^31 - 2^13
  *   counts       dev [B] entries of row b (clamped to [0,N]) or NULL
  *   summary      dev [3]: loss, kl (reduced alike), share of entries whose ratio was clipped
  *   grad_scores  dev [B,N], 0 for entries that take no part
@@ -431,7 +431,8 @@ int fltop_policy_loss(const double* scores, const double* old_scores, const doub
  * numbers of frames that take part have to be finite: what is not, and rows without a finite
  * logit, give what the formulas give.
  * Softmax statistics, exponentials and logarithms are fp32, log-probabilities, their
- * differences and all sums over frames fp64.  Any V >= 1.
+ * differences and all sums over frames fp64.  Any V >= 1 below 2^31 - 2^13, B < 2^24, B * T below
+ * 2^31 - 2^13.
  * workspace: fltop_policy_workspace_bytes(B, T) bytes, 256-byte aligned. */
 int fltop_policy_loss_logits(const fltop_rows* logits, const int32_t* tokens,
                              const float* old_logps, const float* ref_logps,

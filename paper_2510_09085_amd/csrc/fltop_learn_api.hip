@@ -9,19 +9,21 @@ namespace {
 // A launch has fewer than 2^32 threads: of 256 in a workgroup for each row of a batch, of 1024 in two workgroups for each
 // hypothesis, of 256 in four for each block of frames.
 constexpr int64_t kMostBatch = (1 << 24) - 1, kMostHypotheses = (1 << 21) - 1, kMostBlocks = (1 << 22) - 1;
+// Loops over a batch's frames, a row's logits and a row's entries count in 32 bits, up to 8192 beyond the last one.
+constexpr int64_t kMostPlaces = (int64_t)INT32_MAX - 8192;
 
 int check_rows(const fltop_rows* x, bool decodes) {
     if (!x || !x->data || !x->lengths) return FLTOP_ERR_NULL_POINTER;
     if (x->B < 1 || x->T < 1 || x->V < (decodes ? 2 : 1)) return FLTOP_ERR_BAD_SHAPE;
     if (x->batch_stride < 0 || x->frame_stride < 0) return FLTOP_ERR_BAD_SHAPE;
-    if (x->B > kMostBatch || (int64_t)x->B * x->T > (int64_t)INT32_MAX) return FLTOP_ERR_BAD_SHAPE;
+    if (x->B > kMostBatch || (int64_t)x->B * x->T > kMostPlaces || x->V > kMostPlaces) return FLTOP_ERR_BAD_SHAPE;
     if (decodes && x->V > FLTOP_MAX_VOCAB) return FLTOP_ERR_VOCAB_TOO_BIG;
     if (x->type < FLTOP_TYPE_F32 || x->type > FLTOP_TYPE_F16) return FLTOP_ERR_BAD_OPTION;
     return FLTOP_OK;
 }
 
 bool lattice_shapes(int32_t B, int32_t T, int32_t N, int32_t U) {
-    return B >= 1 && T >= 1 && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 && U <= FLTOP_MAX_LABELS &&
+    return B >= 1 && T >= 1 && (int64_t)B * T <= kMostPlaces && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 && U <= FLTOP_MAX_LABELS &&
            (int64_t)B * N <= kMostHypotheses;
 }
 
@@ -113,7 +115,7 @@ extern "C" int fltop_preference_loss(const fltop_preference* p, void* workspace,
 }
 
 extern "C" size_t fltop_policy_workspace_bytes(int32_t B, int32_t T) {
-    if (B < 1 || B > kMostBatch || T < 1 || (int64_t)B * T > (int64_t)INT32_MAX) return 0;
+    if (B < 1 || B > kMostBatch || T < 1 || (int64_t)B * T > kMostPlaces) return 0;
     // (both policy losses are asked for with T = 1: rows of hypotheses, and one token a row)
     const size_t sums = fltop::policy_sums_bytes(B), rows = fltop::row_workspace_bytes(B);
     return sums > rows ? sums : rows;
@@ -124,7 +126,7 @@ extern "C" int fltop_policy_loss(const double* scores, const double* old_scores,
                                  const fltop_policy* policy, void* workspace, size_t workspace_bytes, double* summary,
                                  double* grad_scores, void* hip_stream) {
     if (!scores || !old_scores || !advantages || !summary || !grad_scores) return FLTOP_ERR_NULL_POINTER;
-    if (B < 1 || B > kMostBatch || N < 1) return FLTOP_ERR_BAD_SHAPE;
+    if (B < 1 || B > kMostBatch || N < 1 || N > kMostPlaces) return FLTOP_ERR_BAD_SHAPE;
     int rc = check_policy(policy);
     if (rc != FLTOP_OK) return rc;
     rc = check_space(workspace, workspace_bytes, fltop_policy_workspace_bytes(B, 1));

@@ -36,3 +36,26 @@ def test_policy_workspaces_hold_either_loss(lib, B, T):
         if n < max(over_scores, over_logits):
             assert lib.fltop_policy_loss_logits(ctypes.byref(rows), FAKE, FAKE, None, FAKE, 0, ctypes.byref(policy), FAKE, n,
                                                 FAKE, FAKE, FAKE, None) == SPACE
+
+
+def rows(**change):
+    x = binding.FltopRows(FAKE, FAKE, 10 * 32, 32, 2, 10, 32, 0)
+    for k, v in change.items():
+        setattr(x, k, v)
+    return ctypes.byref(x)
+
+
+@pytest.mark.parametrize("most", [2 ** 31 - 1, 2 ** 31 - 8, 2 ** 31 - 8192])
+def test_counts_that_loops_in_32_bits_would_step_past(lib, most):
+    """Loops go on by up to 8192 behind the last frame, logit or entry."""
+    hyps = binding.FltopHypotheses(FAKE, FAKE, None, 3 * 8, 8, 3, 3, 8)
+    policy = ctypes.byref(binding.FltopPolicy(0, 0, 0.2, 0.2, 0.1, 1.0))
+    long = rows(B=1, T=most, V=2)
+    assert lib.fltop_ctc_score(long, ctypes.byref(hyps), FAKE, None, 0, None) == SHAPE
+    assert lib.fltop_ctc_score_grad(long, ctypes.byref(hyps), FAKE, FAKE, 1 << 62, FAKE, None) == SHAPE
+    for x in (long, rows(B=1, T=1, V=most)):
+        assert lib.fltop_policy_loss_logits(x, FAKE, FAKE, None, FAKE, 0, policy, FAKE, 1 << 62, FAKE, FAKE, FAKE,
+                                            None) == SHAPE
+    assert lib.fltop_policy_loss(FAKE, FAKE, None, FAKE, None, 1, most, policy, FAKE, 1 << 62, FAKE, FAKE, None) == SHAPE
+    assert lib.fltop_policy_workspace_bytes(1, most) == 0
+    assert lib.fltop_policy_workspace_bytes(1, 2 ** 31 - 8193) > 0
