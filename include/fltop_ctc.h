@@ -371,7 +371,8 @@ typedef struct fltop_preference {
     const double*  ref_scores;    /* dev [B,N] or NULL                                            */
     const int32_t* pairs;         /* dev [B,M,2] (won, lost)                                      */
     const int32_t* pair_counts;   /* dev [B] (clamped to [0,M]) or NULL for M each                */
-    int32_t        B, N, M;       /* B < 2^24, N up to FLTOP_MAX_BEAM, M up to 2^29               */
+    int32_t        B, N, M;       /* B < 2^24, N up to FLTOP_MAX_BEAM, M from 1 up to 2^29 (no
+                                     pairs at all: pair_counts of 0)                              */
     int32_t        kind;          /* FLTOP_PREFERENCE_*                                           */
     double         beta;          /* > 0                                                          */
     double         label_smoothing; /* [0, 0.5], sigmoid only (else 0)                            */

@@ -618,7 +618,8 @@ def preference_loss(scores: torch.Tensor, pairs: torch.Tensor, *,
     """fltop_preference_loss: mean loss over pairs (won, lost) of an utterance's hypotheses.
 
     scores, ref_scores float64 [B,N] (ctc_score's), pairs int32 [B,M,2] of places in [0,N) (a pair
-    with any other place takes no part), pair_counts int32 [B]; kind "sigmoid", "hinge" or "square".
+    with any other place takes no part; M may be 0), pair_counts int32 [B]; kind "sigmoid", "hinge"
+    or "square".
     Returns loss (float64), margins [B,M] and grad_scores [B,N], the gradient of scale * loss."""
     _need(scores.is_cuda and scores.dim() == 2, "scores must be a [B,N] device tensor")
     dev, (B, N) = scores.device, scores.shape
@@ -633,17 +634,20 @@ def preference_loss(scores: torch.Tensor, pairs: torch.Tensor, *,
     if kind not in PREFERENCE_KINDS:
         raise ValueError(f"kind must be one of {', '.join(PREFERENCE_KINDS)}")
     with _On(scores, stream) as handle:
+        if M == 0:  # the library takes lists of one pair and more: one that takes no part
+            pairs = torch.full((B, 1, 2), -1, dtype=torch.int32, device=dev)
+        room = pairs.shape[1]
         grad = torch.empty_like(scores)
         loss = torch.empty((), dtype=torch.float64, device=dev)
-        margins = torch.empty((B, M), dtype=torch.float64, device=dev)
+        margins = torch.empty((B, room), dtype=torch.float64, device=dev)
         ws = _workspace(workspace, dev, "fltop_preference_workspace_bytes", B)
         p = FltopPreference(scores.data_ptr(), _address(ref_scores),
                             pairs.data_ptr(), _address(pair_counts),
-                            B, N, M, PREFERENCE_KINDS[kind], beta, label_smoothing, scale,
+                            B, N, room, PREFERENCE_KINDS[kind], beta, label_smoothing, scale,
                             loss.data_ptr(), margins.data_ptr(), grad.data_ptr())
         _raise(load().fltop_preference_loss(ctypes.byref(p), _address(ws), ws.numel(), handle),
                "fltop_preference_loss")
-    return {"loss": loss, "margins": margins, "grad_scores": grad}
+    return {"loss": loss, "margins": margins if M else margins[:, :0], "grad_scores": grad}
 
 
 def _policy(reduction, clip_low, clip_high, kl_weight, scale) -> FltopPolicy:

@@ -277,3 +277,17 @@ def test_a_margin_that_beta_takes_out_of_range(dev, B):
     for smoothed in (won, won.flip(2).contiguous()):
         out = binding.preference_loss(s, smoothed, beta=1e10, label_smoothing=0.25)
         assert float(out["loss"]) == math.inf and torch.isfinite(out["grad_scores"]).all()
+
+
+@pytest.mark.parametrize("B", [1, 3, 3000])
+def test_lists_without_pairs(dev, B):
+    """A batch of which nothing can be paired: no loss, no gradient, no margins."""
+    s = -10 * torch.rand((B, 4), dtype=torch.float64, device=dev)
+    none = torch.empty((B, 0, 2), dtype=torch.int32, device=dev)
+    for more in ({}, {"pair_counts": torch.zeros(B, dtype=torch.int32, device=dev)},
+                 {"pair_counts": torch.full((B,), 7, dtype=torch.int32, device=dev), "kind": "square", "ref_scores": s}):
+        out = binding.preference_loss(s, none, **more)
+        assert float(out["loss"]) == 0.0 and out["margins"].shape == (B, 0)
+        assert out["grad_scores"].shape == s.shape and not out["grad_scores"].any()
+    with pytest.raises(binding.FltopError):
+        binding.preference_loss(s, none, beta=-1.0)
