@@ -462,6 +462,10 @@ def stats_dict(stats: torch.Tensor) -> dict:
 
 
 # ---- learning from hypotheses ------------------------------------------------------------------
+#
+# Calls on plain device memory, as decode is: nothing that they return carries autograd history, also
+# where an input requires a gradient.  Gradients are results of their own (grad_scores, grad_logits,
+# ctc_score_grad's) and reach a model by `tensor.backward(gradient)`.
 
 ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 PREFERENCE_KINDS = {"sigmoid": 0, "hinge": 1, "square": 2}
@@ -576,7 +580,9 @@ def ctc_score(logprobs: torch.Tensor, lengths: torch.Tensor, tokens: torch.Tenso
     transposed is fine), lengths [B]; tokens [B,N,U] and token_lengths [B,N] int32 as decode's
     n-best export gives them (slices too: `nbest_tokens[:, :8, :200]`), counts [B] its nbest_count.
     Returns scores [B,N] float64; with want_grad also the workspace that ctc_score_grad needs
-    (about 4 * B * N * T * U bytes: slice the tokens to the longest hypothesis)."""
+    (about 4 * B * N * T * U bytes, twice that from U = 1920 on: slice the tokens to the longest
+    hypothesis).  The scores carry no autograd history, whether or not logprobs does: their gradient is
+    what ctc_score_grad returns."""
     x = _rows(logprobs, lengths, "logprobs")
     dev = logprobs.device
     h = _hypotheses(tokens, token_lengths, counts, x.B, dev)

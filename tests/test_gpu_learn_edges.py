@@ -291,3 +291,18 @@ def test_lists_without_pairs(dev, B):
         assert out["grad_scores"].shape == s.shape and not out["grad_scores"].any()
     with pytest.raises(binding.FltopError):
         binding.preference_loss(s, none, beta=-1.0)
+
+
+def test_inputs_that_require_a_gradient(dev):
+    """They are read as they are; what comes back carries no history, and backward(gradient) goes on from it."""
+    logits = torch.randn((2, 20, 12), generator=torch.Generator(device=dev).manual_seed(1), device=dev, requires_grad=True)
+    x = torch.log_softmax(logits, 2)
+    lengths = torch.tensor([20, 13], dtype=torch.int32, device=dev)
+    tok = torch.randint(1, 12, (2, 1, 5), device=dev).to(torch.int32)
+    tl = torch.full((2, 1), 5, dtype=torch.int32, device=dev)
+    out = binding.ctc_score(x, lengths, tok, tl, want_grad=True)
+    grad = binding.ctc_score_grad(x, lengths, tok, tl, torch.ones_like(out["scores"]), out["workspace"])
+    assert not out["scores"].requires_grad and not grad.requires_grad
+    x.backward(grad)
+    plain = binding.ctc_score(x.detach(), lengths, tok, tl)["scores"]
+    assert torch.equal(out["scores"], plain) and logits.grad is not None and logits.grad.any()
