@@ -107,7 +107,7 @@ struct ScoreSpace {
 
 // Pairs of states that a lane holds where a direction has a workgroup of its own: two while that has sixteen wavefronts at
 // most, with the one that tabulates.  (With eight pairs the registers spill: 16 transcripts of 1700 tokens over 3600 frames
-// took 12.5 ms, both directions at once, and take 5.7 ms now.)
+// of an untrained model took 12.5 ms, both directions at once, and take 5.4 ms now, 5.7 with the borders for a gradient.)
 inline int lattice_pairs(int32_t U) { return U < 1920 ? 2 : 4; }
 inline int waves_for(int32_t U, int pairs) { return (U + 64 * pairs) / (64 * pairs); }   // for U + 1 pairs
 // Frames that are gone through together: exponents are kept once for each such block.

@@ -23,8 +23,8 @@ int check_rows(const fltop_rows* x, bool decodes) {
 }
 
 bool lattice_shapes(int32_t B, int32_t T, int32_t N, int32_t U) {
-    return B >= 1 && T >= 1 && (int64_t)B * T <= kMostPlaces && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 && U <= FLTOP_MAX_LABELS &&
-           (int64_t)B * N <= kMostHypotheses;
+    return B >= 1 && T >= 1 && (int64_t)B * T <= kMostPlaces && N >= 1 && N <= FLTOP_MAX_BEAM && U >= 1 &&
+           U <= FLTOP_MAX_LABELS && (int64_t)B * N <= kMostHypotheses;
 }
 
 // Whether the borders of these lattices can be addressed (their places as bytes within 63 bits), and their blocks launched.

@@ -391,7 +391,8 @@ hipError_t launch_preference(const fltop_preference& p, void* workspace, hipStre
     PairSums* sums = static_cast<PairSums*>(workspace);
     const int64_t scores = (int64_t)p.B * p.N, pairs = (int64_t)p.B * p.M;
     if (scores <= kOneScores && pairs <= kOnePairs) {
-        hipLaunchKernelGGL(preference_one_kernel, dim3(1), dim3(kOneThreads), (size_t)scores * 16 + (size_t)p.B * 8, stream, p);
+        hipLaunchKernelGGL(preference_one_kernel, dim3(1), dim3(kOneThreads), (size_t)scores * 16 + (size_t)p.B * 8, stream,
+                           p);
         return hipGetLastError();
     }
     // 128 utterances of 4950 pairs: 29 us with 256 threads, 20 us with 1024, about half of which are the exponentials and

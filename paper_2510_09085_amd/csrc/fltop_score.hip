@@ -43,9 +43,11 @@ __device__ inline Hyp hypothesis(const fltop_rows& x, const fltop_hypotheses& h,
 // (below); a second kernel then goes through the blocks of all utterances at once, once more from either border, and needs
 // no masses of single frames in memory.
 //
-// The serial frames bound it: 64 transcripts of 500 frames take 79 us, 63 blocks at about 1.2 us each, of which the five
+// The serial frames bound it: 64 transcripts of 500 frames take 77 us, 63 blocks at about 1.2 us each, of which the five
 // products and sums of a frame's two pairs are a third; the rest are the latencies of the barrier, of LDS, of the lanes'
-// exponents and of the shifts.  2048 hypotheses of 500 frames keep all compute units busy and take 270 us.
+// exponents and of the shifts (counted: vector instructions issue in a third of a wavefront's life, any in 58%).  2048
+// hypotheses of 500 frames keep all compute units busy and take 245 us, in half of which the SIMDs issue a vector
+// instruction.
 //
 // Frames come in blocks of R.  Within a block only l_{i-1} passes from lane to lane (one DPP shift),
 // and the wavefront above takes the same block one turn later with the last lane's masses from LDS,
@@ -829,8 +831,9 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(WAVES))
 // whole numbers: in any order the same.  One exponent for each lane does wherever P's is within reach of it (kMostShift).
 //
 // About a thousand vector instructions a chunk and block, and loads of the borders that depend on the hypothesis's length,
-// which is loaded before: 64 transcripts of 500 frames take 28 us, 256 of up to 1500 frames 290 us, where the borders'
-// 0.6 GB alone are 120 us.  Four wavefronts a SIMD, the most that registers allow, are worth more than a few spills.
+// which is loaded before: 64 transcripts of 500 frames take 26 us, 256 of up to 1500 frames 252 us, in two thirds of
+// which the SIMDs issue a vector instruction; the borders' 0.36 GB alone are 73 us.  Four wavefronts a SIMD, the most that
+// registers allow, are worth more than a few spills.
 
 constexpr int kGradPairs = 2, kGradThreads = 256;   // (at most)
 
@@ -1186,7 +1189,8 @@ hipError_t score_as(const fltop_rows& x, const fltop_hypotheses& h, double* out_
                     hipStream_t stream) {
     // Registers for three wavefronts a SIMD, so that a table's exponentials can be read ahead, where a direction has four at
     // most and the hypotheses do not fill the chip twice (64 transcripts of 229 tokens: 79 us, 86 with the other build); else
-    // for four (2048 hypotheses of 229: 269 us, 345 with the first).
+    // for four (2048 hypotheses of 229: 269 us, 345 with the first).  This and all that follows goes by the room for tokens,
+    // which the host knows, not by the hypotheses' lengths, which it does not.
     const bool few = h.U < 512 && (int64_t)x.B * h.N < 512;
     if (!keep && h.U < 896) {
         if (few) return score_with<2, 4, 8, 3, TABLE, false>(x, h, out_scores, keep, stream);
@@ -1208,8 +1212,9 @@ hipError_t grad_as(const fltop_rows& x, const fltop_hypotheses& h, const double*
     const int32_t blocks = (int32_t)blocks_of(x.T, R);
     const size_t bytes = (size_t)R * width * 8 + (TABLE ? R * kTabulated * 8 : 0);
     // With a table one wavefront for six chunks: shorter hypotheses than the longest leave none idle, and the others' loads
-    // go on while one waits (64 transcripts: 40 us with a wavefront for each of 3 chunks, 28 with one for all; 256 of up to
-    // 7 chunks: 422 with four, 287 with one; 32 x 4 hypotheses: 47 with four, 42 with two, 55 with one).  Without one as many
+    // go on while one waits.  With one, two and four wavefronts, in us: 64 x 500 frames of 3 chunks 27, 30, 43; 256 x 1500 of
+    // 7 chunks 613, 650, 825; 64 x 1000 of 10 130, 135, 148; 32 x 500 of 12 47, 39, 45; 16 x 500 of 24 71, 48, 41; 8 x 500 of
+    // 96 250, 156, 95 (where 8 chunks are eight short hypotheses, 46, 38, 42, the rule takes one).  Without a table as many
     // as there may be chunks, which share the block's long rows of sums (32 x 8: 212 us with one, 127 with two, 80 with four).
     const int64_t chunks = (int64_t)h.N * ((h.U + 1) / (kWave * kGradPairs - 2 * R) + 1);
     const int64_t waves = TABLE ? chunks / 6 : chunks, most = kGradThreads / kWave;
