@@ -887,7 +887,10 @@ struct Chunk {
         }
     }
 
-    // One exponent for the lane's masses and those that may reach it, and that of the lane which they come from.
+    // One exponent for the lane's masses and those that may reach it, and that of the lane which they come from.  From a mass
+    // at one border to the one at the other that an alignment goes on with it is R + 1 pairs, a step for each frame and one
+    // to the frame behind: every lane on that way counts both, so that none of them takes an exponent by what is of no
+    // use to the alignment and finds its masses too small to hold, while no sum of exponents tells of it.
     template <bool UP>
     __device__ static void window(const Mass (&b)[K], const Mass (&l)[K], int32_t* E, int32_t* beside) {
         int32_t top = kNoMass;
@@ -895,7 +898,7 @@ struct Chunk {
         for (int k = 0; k < K; ++k) top = max(top, max(b[k].e, l[k].e));
         int32_t m = top;
 #pragma unroll
-        for (int d = 0; d < (R + K - 1) / K; ++d) m = max(UP ? from_below(m, kNoMass) : from_above(m, kNoMass), top);
+        for (int d = 0; d < (R + K) / K; ++d) m = max(UP ? from_below(m, kNoMass) : from_above(m, kNoMass), top);
         *E = m;
         *beside = UP ? from_below(m, kNoMass) : from_above(m, kNoMass);
     }

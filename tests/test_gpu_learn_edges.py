@@ -306,3 +306,31 @@ def test_inputs_that_require_a_gradient(dev):
     x.backward(grad)
     plain = binding.ctc_score(x.detach(), lengths, tok, tl)["scores"]
     assert torch.equal(out["scores"], plain) and logits.grad is not None and logits.grad.any()
+
+
+@pytest.mark.parametrize("cost", [400.0, 900.0, 5000.0])
+@pytest.mark.parametrize("L,U,V", [(40, 40, 60), (40, 40, 90), (140, 140, 60), (40, 1920, 60), (40, 1920, 90), (140, 1920, 90)])
+def test_one_costly_token_among_as_many_as_there_are_frames(dev, L, U, V, cost):
+    """As many frames as tokens: one alignment, a new token in each frame, whatever the emissions are.  One of the tokens,
+    another one for each utterance, costs e^-cost in every frame, so that what lies above it at a border of a block is that
+    much likelier to get to the end than what the alignment has there."""
+    B = L
+    word = 1 + np.arange(L) % (V - 2)   # (no two neighbours alike)
+    lp = np.full((B, L, V), -2.0, np.float32)
+    for b in range(B):
+        lp[b, :, word[b]] = -cost
+    tok = np.ones((B, 1, U), np.int32)
+    tok[:, 0, :L] = word
+    x = torch.from_numpy(lp).to(dev)
+    args = [torch.from_numpy(a).to(dev) for a in (np.full(B, L, np.int32), tok, np.full((B, 1), L, np.int32))]
+    out = binding.ctc_score(x, *args, want_grad=True)
+    grad = binding.ctc_score_grad(x, *args, torch.ones((B, 1), dtype=torch.float64, device=dev), out["workspace"])
+    total = lp[:, np.arange(L), word].astype(np.float64).sum(1)
+    want = np.zeros((L, V))
+    want[np.arange(L), word] = 1.0
+    for b in range(B):
+        assert abs(float(out["scores"][b, 0]) - total[b]) <= ref.score_tolerance(L, total[b]), b
+    got = grad.double().cpu().numpy()
+    near = ref.grad_tolerance("f32", L, want[None], want[None], np.array([2.0 * L + 1]))[0]
+    off = [b for b in range(B) if np.any(np.abs(got[b] - want) > near)]
+    assert not off, off
