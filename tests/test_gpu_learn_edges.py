@@ -60,8 +60,8 @@ def log_lattice(lp, tokens):
     e = lp.astype(np.float64)[:, z]
     S = len(z)
     skip = np.where((np.arange(S) > 1) & (z != 0) & (z != np.roll(z, 2)), 0.0, -np.inf)
-    up = lambda x, by: np.concatenate((np.full(by, -np.inf), x[:-by]))  # noqa: E731
-    down = lambda x, by: np.concatenate((x[by:], np.full(by, -np.inf)))  # noqa: E731
+    up = lambda x, by: np.concatenate((np.full(by, -np.inf), x))[:S]  # noqa: E731
+    down = lambda x, by: np.concatenate((x, np.full(by, -np.inf)))[by:]  # noqa: E731
     with np.errstate(invalid="ignore"):
         a = [np.where(np.arange(S) < 2, e[0], -np.inf)]
         for t in range(1, len(lp)):
@@ -70,7 +70,7 @@ def log_lattice(lp, tokens):
         for t in range(len(lp) - 2, -1, -1):
             y = b[-1] + e[t + 1]
             b.append(np.logaddexp(np.logaddexp(y, down(y, 1)), down(y + skip, 2)))
-        total = np.logaddexp(a[-1][-1], a[-1][-2])
+        total = np.logaddexp(a[-1][-1], a[-1][-2]) if S > 1 else a[-1][-1]
         share = np.exp(np.array(a) + np.array(b[::-1]) - total)
     out = np.zeros(lp.shape)
     np.add.at(out.T, z, share.T)
@@ -334,3 +334,44 @@ def test_one_costly_token_among_as_many_as_there_are_frames(dev, L, U, V, cost):
     near = ref.grad_tolerance("f32", L, want[None], want[None], np.array([2.0 * L + 1]))[0]
     off = [b for b in range(B) if np.any(np.abs(got[b] - want) > near)]
     assert not off, off
+
+
+@pytest.mark.parametrize("kind", ["steep", "heavy tails", "costly tokens", "levels", "masked"])
+@pytest.mark.parametrize("L,U,V,T", [(0, 1, 5, 9), (7, 7, 12, 7), (63, 70, 32, 71), (64, 64, 80, 64), (112, 113, 32, 121),
+                                     (128, 128, 65, 131), (129, 1000, 20, 150), (128, 2004, 65, 138), (256, 1920, 12, 259)])
+def test_emissions_of_mixed_regimes(dev, kind, L, U, V, T):
+    """Masses that lie far apart in some lanes and not in others, with little room for alignments: both ways through a block
+    side by side, scores with and without the borders, and the gradient."""
+    gen = torch.Generator().manual_seed(L + V + len(kind))
+    x = torch.randn((2, T, V), generator=gen)
+    if kind == "steep":
+        x = torch.full((2, T, V), -36.0)
+        x[:, :, 0] = -0.001
+        x[1, T // 2:, 0] = -39.0
+    elif kind == "heavy tails":
+        x = torch.log_softmax(x / torch.randn((2, T, V), generator=gen).abs().clamp_min(1e-3), 2)
+    elif kind == "costly tokens":
+        x = x - 900.0 * (torch.rand((2, 1, V), generator=gen) < 0.2) * torch.rand((2, 1, V), generator=gen)
+    elif kind == "levels":
+        x = x + 100.0 * (torch.rand((2, T, 1), generator=gen) - 0.7)
+    else:
+        x = torch.log_softmax(x, 2).masked_fill(torch.rand((2, T, V), generator=gen) < 0.005, -math.inf)
+    tok = (1 + (torch.arange(U) + torch.randint(0, V, (2, 1, 1), generator=gen)) % (V - 1)).expand(2, 1, U).to(torch.int32)
+    lengths, tl = torch.tensor([T, max(T - 2, min(T, L))]), torch.tensor([[L], [max(0, L - 1)]])
+    args = [x.to(dev)] + [a.to(torch.int32).contiguous().to(dev) for a in (lengths, tok, tl)]
+    out = binding.ctc_score(*args, want_grad=True)
+    alone = binding.ctc_score(*args)["scores"]
+    grad = binding.ctc_score_grad(*args, torch.ones((2, 1), dtype=torch.float64, device=dev), out["workspace"])
+    for b in range(2):
+        n, frames = int(tl[b, 0]), int(lengths[b])
+        want, share = log_lattice(x[b, :frames].numpy(), tok[b, 0, :n].numpy())
+        got = grad[b].double().cpu().numpy()
+        if not np.isfinite(want):
+            assert float(out["scores"][b, 0]) == -math.inf and float(alone[b, 0]) == -math.inf and not got.any()
+            continue
+        # the reference's own: each frame adds numbers of the score's size a few times, each time half a step of that off
+        slack = 4 * T * 2.0 ** -53 * max(abs(want), 1.0)
+        for s in (out["scores"], alone):
+            assert abs(float(s[b, 0]) - want) <= slack + ref.score_tolerance(T, want)
+        near = ref.grad_tolerance("f32", T, share[None], share[None], np.array([2.0 * n + 1]))[0] + 4 * slack * share
+        assert np.all(np.abs(got[:frames] - share) <= near) and not got[frames:].any()
